@@ -54,7 +54,10 @@ typedef struct s3_arena s3_arena; /* opaque; host-side metadata owned by the lib
 
 /* S3_E4M3: 8-bit float, 1 sign / 4 exponent (bias 7) / 3 fraction bits, no infinities, largest 448
  * (cache rows only; related work: quantisation as a complementary way to shrink the cache). */
-typedef enum { S3_F16 = 0, S3_BF16 = 1, S3_F32 = 2, S3_E4M3 = 3 } s3_dtype;
+/* S3_MXFP4: 4-bit floats, 1 sign / 2 exponent (bias 1) / 1 fraction bit (0, 0.5, 1, 1.5, 2, 3, 4, 6), in blocks of 32
+ * consecutive elements of a head under one power of two, 2^(byte - 127) (the open microscaling format; cache rows only).  4 1/4
+ * bits an element.  (4 names no type.) */
+typedef enum { S3_F16 = 0, S3_BF16 = 1, S3_F32 = 2, S3_E4M3 = 3, S3_MXFP4 = 5 } s3_dtype;
 
 typedef enum {
     S3_OK = 0,
@@ -73,21 +76,27 @@ typedef struct {
     int32_t head_dim;  /* D: 64, 128 or 256; 96 for multi-head 16-bit caches (n_kv_heads 0 or
                           n_heads, kv_dtype S3_F16 / S3_BF16)                            */
     int32_t kv_dtype;  /* s3_dtype of the cache rows (and, if 16-bit, of q, k_new, v_new):
-                          S3_F16, S3_BF16 or S3_E4M3                                     */
+                          S3_F16, S3_BF16, S3_E4M3 or S3_MXFP4                           */
     int32_t granule;   /* G: capacities are multiples of G tokens (> 0)                  */
     int32_t max_len;   /* M: largest capacity, tokens; a multiple of G                   */
     int32_t n_kv_heads; /* heads of K and V: 0 or n_heads = one per query head; a divisor of n_heads =
                            grouped-query, 1 = multi-query attention (each K/V head serves
                            n_heads / n_kv_heads query heads; q and out keep n_heads)       */
-    int32_t act_dtype; /* kv_dtype == S3_E4M3 only: type of q, k_new, v_new, S3_F16 or S3_BF16 (append
-                          rounds a new row to the nearest e4m3 code, ties to even, saturating at
+    int32_t act_dtype; /* kv_dtype == S3_E4M3 or S3_MXFP4 only: type of q, k_new, v_new, S3_F16 or S3_BF16
+                          (append rounds a new row to the nearest e4m3 code, ties to even, saturating at
                           +-448, NaN -> 0x7f; attention widens the codes exactly).  Ignored for 16-bit
                           caches.  s3_kv_fill and s3_kv_read_rows move codes (one byte per
-                          element).                                                       */
+                          element).
+                          S3_MXFP4: a block's scale is the least power of two under which its largest
+                          magnitude is below 7 (at most 2^125; S3_F16: 2^13), its codes the nearest, ties to
+                          even, 6 at the most; a block with an infinity or a NaN has scale byte 255 and reads
+                          as NaN.  s3_kv_fill and s3_kv_read_rows move stored rows: the codes of all heads,
+                          [n_kv_heads][head_dim / 2] bytes (element 2i in the low half of byte i), the scale
+                          bytes [n_kv_heads][head_dim / 32], zeros up to a multiple of 16 bytes.       */
 } s3_kv_config;
 
 /* KV-cache bytes one token occupies: 2 * n_layers * n_kv_heads * head_dim * sizeof(element)
- * (section 2.1: 4*l*d_h bytes in half precision).  Returns the byte count, or
+ * (section 2.1: 4*l*d_h bytes in half precision; S3_MXFP4: 2 * n_layers stored rows).  Returns the byte count, or
  * S3_ERR_INVALID (< 0) for a bad config. */
 int64_t s3_kv_bytes_per_token(const s3_kv_config *cfg /*HOST*/);
 
@@ -145,7 +154,7 @@ int s3_kv_slot_info(const s3_arena *a, int32_t slot_id, int64_t *off /*HOST*/, i
  *             its reservation: call s3_kv_grow), anything else bad gives S3_ERR_INVALID; in
  *             both cases nothing is written.  When NULL the caller vouches for the positions.
  *   slot_off  DEVICE [n] int64, pos DEVICE [n] int32
- *   k_new, v_new  DEVICE [n][H][D] elements of kv_dtype (8-bit caches: of act_dtype, quantised here;
+ *   k_new, v_new  DEVICE [n][H][D] elements of kv_dtype (8-bit and 4-bit caches: of act_dtype, quantised here;
  *                 shared K/V heads: [n][n_kv_heads][D]), 16-byte aligned */
 int s3_kv_append(s3_arena *a, int32_t layer, int32_t n, const int32_t *slot_id, const int32_t *pos_host,
                  const int64_t *slot_off, const int32_t *pos, const void *k_new, const void *v_new,
@@ -159,7 +168,7 @@ int s3_kv_append(s3_arena *a, int32_t layer, int32_t n, const int32_t *slot_id, 
  * the vector-ALU kernel of shared heads, where a second kernel does.  (An infinite cached value makes its
  * output element infinite or NaN; NaN always with four and more query heads per cached head, whose weighted
  * sum runs over weights split into two 16-bit parts.)
- *   q         DEVICE [n][H][D] kv_dtype (8-bit caches: act_dtype), 16-byte aligned
+ *   q         DEVICE [n][H][D] kv_dtype (8-bit and 4-bit caches: act_dtype), 16-byte aligned
  *   slot_off  DEVICE [n] int64, cur_len DEVICE [n] int32
  *   out       DEVICE [n][H][D] of out_dtype (S3_F32, S3_F16 or S3_BF16), 16-byte aligned
  *   scale     <= 0 means 1/sqrt(D)
@@ -177,11 +186,61 @@ int s3_decode_attention(s3_arena *a, int32_t layer, int32_t n, const void *q, co
  *             be the same array as pos (S3_ERR_INVALID) - alternate between two arrays. */
 /* (Shared key/value heads: the same call, results and checks, as one to three launches on `stream`: the
  * append (folded into the attention kernel when the matrix-core kernel runs, but for large batches of 8-bit rows), the
- * attention kernel, and, with the vector-ALU kernel, a merge of chunk partials.  An 8-bit multi-head cache rounds the new row
- * to codes in the same kernel that attends over it.) */
+ * attention kernel, and, with the vector-ALU kernel, a merge of chunk partials.  An 8-bit multi-head cache and a 4-bit cache, of
+ * shared heads too, round the new row to codes in the same kernel that attends over it.) */
 int s3_decode_step(s3_arena *a, int32_t layer, int32_t n, const int32_t *slot_id, const int32_t *pos_host,
                    const int64_t *slot_off, const int32_t *pos, const void *q, const void *k_new,
                    const void *v_new, void *out, int32_t out_dtype, float scale, int32_t *len_out, void *stream);
+
+/* How queries and keys are treated before they are used: each head's norm, then its rotation by the token's position.
+ *   norm      x * 1 / sqrt(mean(x^2) + eps) * weight over the head_dim elements of a head, if a weight is given
+ *   rotation  pair i of the first rotary_dim elements, (i, i + rotary_dim/2) or, interleaved, (2i, 2i+1), turns from (a, b) to
+ *             (a cos t - b sin t, a sin t + b cos t), t = position * inv_freq[i]; elements from rotary_dim on are not turned
+ * Norms, angles and rotation are computed in 32 bits (angles from positions far out in 64) and rounded once.
+ * Several axes (time, height, width): pair i turns by the token's position on axis axis_of_pair[i]. */
+typedef struct {
+    int32_t rotary_dim;   /* even, 0 (no rotation) .. head_dim                                                    */
+    int32_t interleaved;  /* 0: pairs (i, i + rotary_dim/2), 1: pairs (2i, 2i+1)                                   */
+    int32_t n_axes;       /* position axes, 1 .. 4                                                                 */
+    float eps;            /* of the norms, >= 0                                                                    */
+    const float *inv_freq;         /* DEVICE [rotary_dim/2] radians per position                                   */
+    const uint8_t *axis_of_pair;   /* HOST [rotary_dim/2], each < n_axes; NULL with one axis                       */
+    const float *q_weight, *k_weight; /* DEVICE [head_dim] or NULL: that norm is left out                          */
+} s3_rotary;
+
+/* Norms and rotation of n tokens' queries and keys, in one pass, without a cache.
+ *   dtype      S3_F16 or S3_BF16, of q, k and the outputs; head_dim 64, 96, 128 or 256
+ *   rot_pos    DEVICE [n_axes][n] positions, any value
+ *   q, k       DEVICE, 16-byte aligned, n rows of [n_heads][head_dim] / [n_kv_heads][head_dim] elements, q_stride / k_stride
+ *              elements from row to row (0: dense; else a multiple of 8, at least a row: a part of a joined projection).  Either may be
+ *              NULL (with its output): nothing is done for it.
+ *   q_out, k_out  DEVICE, 16-byte aligned, strides as q and k; may be q and k themselves (in place), no other overlap */
+int s3_qk_rotary(const s3_rotary *rule /*HOST*/, int32_t dtype, int32_t head_dim, int32_t n, const int32_t *rot_pos, const void *q,
+                 int32_t n_heads, int64_t q_stride, const void *k, int32_t n_kv_heads, int64_t k_stride, void *q_out, void *k_out,
+                 void *stream);
+
+/* s3_kv_append with norms and rotation on the way, in one pass over the projections of n new tokens: keys are normed, turned and
+ * written (rounded once, to the cache's type or codes), values written as s3_kv_append writes them, queries normed, turned and
+ * written to q_out, dense [n][n_heads][head_dim] as s3_decode_attention takes them.  A token is an entry of slot_off / pos, as in
+ * s3_kv_append: single tokens of a batch, whole prompts (a run of entries with one slot's offset) or a mix; rows of one
+ * call must differ.  Entries that s3_kv_append would skip (off < 0 marks padding) write nothing, to q_out neither.
+ *   slot_id, pos_host  as in s3_kv_append
+ *   rot_pos    DEVICE [n_axes][n] positions for the rotation, or NULL: pos, on every axis
+ *   q          DEVICE rows of [n_heads][head_dim], or NULL (q_out is not used then); q_out == q only with dense rows
+ *   k_new, v_new  DEVICE rows of [n_kv_heads][head_dim]; strides in elements as in s3_qk_rotary; all of act_dtype (16-bit caches:
+ *              kv_dtype), 16-byte aligned */
+int s3_kv_append_rotary(s3_arena *a, int32_t layer, int32_t n, const int32_t *slot_id, const int32_t *pos_host,
+                        const int64_t *slot_off, const int32_t *pos, const s3_rotary *rule /*HOST*/, const int32_t *rot_pos,
+                        const void *q, int64_t q_stride, const void *k_new, int64_t k_stride, const void *v_new, int64_t v_stride,
+                        void *q_out, void *stream);
+
+/* The inverse of s3_kv_append: for b in [0, n) the key and value of `layer` in row pos[b] of the slot at slot_off[b], as numbers of
+ * the type of new rows (8-bit and 4-bit codes widened; a power of two that the type does not reach becomes an infinity or loses
+ * bits, which no appended row does).  For a prompt's own attention over cached rows, or to look at a quantised cache.
+ *   k_out, v_out  DEVICE [n][n_kv_heads][head_dim], 16-byte aligned; one of them may be NULL.  Entries that attention would refuse
+ *                 are left as they are. */
+int s3_kv_fetch(s3_arena *a, int32_t layer, int32_t n, const int64_t *slot_off, const int32_t *pos, void *k_out, void *v_out,
+                void *stream);
 
 /* For callers that cannot allocate device memory: code recorded into a HIP graph, serving loops that must
  * never synchronise, harnesses that forbid hipMalloc.  Exactly s3_decode_step (same arguments, checks,
@@ -355,7 +414,7 @@ int s3_kv_probe_bandwidth(s3_arena *a, size_t bytes, int32_t mode, int32_t reps,
  * get names: the above plus "default_variant", "kernel_kind" (0 multi-head kernels, 1 shared-K/V vector-ALU kernel
  * (with nothing set by the caller the matrix-core kernel takes its place for the batches that it serves faster),
  * 2 shared-K/V matrix-core kernel, 3 kernel for 8-bit rows, 4 matrix-core kernel over 8-bit rows with
- * shared heads: what the next attention launch uses), "n_variants", "n_grows",
+ * shared heads, 5 kernel for rows of 4-bit blocks: what the next attention launch uses), "n_variants", "n_grows",
  * "live_slots", "scratch_bytes", "num_cus" and,
  * after "profile" k, "profile_launches", "profile_partial_ns", "profile_merge_ns" (sums over the
  * timed launches since the last reset) and "profile_p10_ns", "profile_p50_ns", "profile_p90_ns"

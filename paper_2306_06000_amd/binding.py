@@ -14,7 +14,7 @@ import sysconfig
 
 import numpy as np
 
-S3_F16, S3_BF16, S3_F32, S3_E4M3 = 0, 1, 2, 3
+S3_F16, S3_BF16, S3_F32, S3_E4M3, S3_MXFP4 = 0, 1, 2, 3, 5
 S3_OK, S3_ERR_INVALID, S3_ERR_NOMEM, S3_ERR_SLOT_FULL, S3_ERR_MAXLEN, S3_ERR_HIP, S3_ERR_SCRATCH = 0, -1, -2, -3, -4, -5, -6
 S3_STATIC_SCRATCH_BYTES = 32 << 20
 
@@ -31,6 +31,12 @@ class s3_kv_config(ctypes.Structure):
                 ("n_kv_heads", ctypes.c_int32), ("act_dtype", ctypes.c_int32)]
 
 
+class s3_rotary(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("n_axes", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("inv_freq", ctypes.c_void_p), ("axis_of_pair", ctypes.c_void_p), ("q_weight", ctypes.c_void_p),
+                ("k_weight", ctypes.c_void_p)]
+
+
 _vp, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
 _pi32, _pi64 = ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int64)
 
@@ -45,6 +51,10 @@ SIGNATURES = {
     "s3_kv_free": (ctypes.c_int, [_vp, _i32]),
     "s3_kv_slot_info": (ctypes.c_int, [_vp, _i32, _pi64, _pi32]),
     "s3_kv_append": (ctypes.c_int, [_vp, _i32, _i32, _pi32, _pi32, _vp, _vp, _vp, _vp, _vp]),
+    "s3_qk_rotary": (ctypes.c_int, [ctypes.POINTER(s3_rotary), _i32, _i32, _i32, _vp, _vp, _i32, _i64, _vp, _i32, _i64, _vp, _vp, _vp]),
+    "s3_kv_append_rotary": (ctypes.c_int, [_vp, _i32, _i32, _pi32, _pi32, _vp, _vp, ctypes.POINTER(s3_rotary), _vp, _vp, _i64, _vp, _i64,
+                                           _vp, _i64, _vp, _vp]),
+    "s3_kv_fetch": (ctypes.c_int, [_vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp]),
     "s3_decode_attention": (ctypes.c_int, [_vp, _i32, _i32, _vp, _vp, _vp, _vp, _i32, _f32, _vp]),
     "s3_decode_step": (ctypes.c_int, [_vp, _i32, _i32, _pi32, _pi32, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _f32, _vp, _vp]),
     "s3_decode_step_static": (ctypes.c_int, [_vp, _i32, _i32, _pi32, _pi32, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _f32, _vp, _vp]),
@@ -194,6 +204,41 @@ def s3_kv_append(arena, layer, n, slot_off, pos, k_new, v_new, stream=0, slot_id
     _b, php = _host_i32(pos_host)
     return lib().s3_kv_append(arena, int(layer), int(n), idp, php, _ptr(slot_off), _ptr(pos), _ptr(k_new),
                               _ptr(v_new), stream or None)
+
+
+def make_rotary(rotary_dim, inv_freq, interleaved=False, n_axes=1, axis_of_pair=None, q_weight=None, k_weight=None, eps=1e-6):
+    """The rule of s3_qk_rotary and s3_kv_append_rotary.  inv_freq, q_weight, k_weight: float32 device tensors (or addresses);
+    axis_of_pair: host sequence.  The rule keeps them alive."""
+    axis = None if axis_of_pair is None else np.ascontiguousarray(axis_of_pair, np.uint8)
+    if axis is not None and axis.size < int(rotary_dim) // 2:
+        raise ValueError(f"axis_of_pair holds {axis.size} of {int(rotary_dim) // 2} pairs")
+    for name, t, size in (("inv_freq", inv_freq, int(rotary_dim) // 2), ("q_weight", q_weight, 1), ("k_weight", k_weight, 1)):
+        if hasattr(t, "data_ptr") and (str(t.dtype) != "torch.float32" or t.numel() < size or not t.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous float32 with at least {size} elements")
+    rule = s3_rotary(int(rotary_dim), int(interleaved), int(n_axes), float(eps), _ptr(inv_freq), _ptr(axis), _ptr(q_weight), _ptr(k_weight))
+    rule.keep = (inv_freq, axis, q_weight, k_weight)
+    return rule
+
+
+def _rule(rule):
+    return None if rule is None else ctypes.byref(rule)
+
+
+def s3_qk_rotary(rule, dtype, head_dim, n, rot_pos, q, n_heads, k, n_kv_heads, q_out, k_out, q_stride=0, k_stride=0, stream=0):
+    return lib().s3_qk_rotary(_rule(rule), int(dtype), int(head_dim), int(n), _ptr(rot_pos), _ptr(q), int(n_heads), int(q_stride), _ptr(k),
+                              int(n_kv_heads), int(k_stride), _ptr(q_out), _ptr(k_out), stream or None)
+
+
+def s3_kv_append_rotary(arena, layer, n, slot_off, pos, rule, q, k_new, v_new, q_out, rot_pos=None, q_stride=0, k_stride=0, v_stride=0,
+                        stream=0, slot_id=None, pos_host=None):
+    _a, idp = _host_i32(slot_id)
+    _b, php = _host_i32(pos_host)
+    return lib().s3_kv_append_rotary(arena, int(layer), int(n), idp, php, _ptr(slot_off), _ptr(pos), _rule(rule), _ptr(rot_pos), _ptr(q),
+                                     int(q_stride), _ptr(k_new), int(k_stride), _ptr(v_new), int(v_stride), _ptr(q_out), stream or None)
+
+
+def s3_kv_fetch(arena, layer, n, slot_off, pos, k_out, v_out, stream=0):
+    return lib().s3_kv_fetch(arena, int(layer), int(n), _ptr(slot_off), _ptr(pos), _ptr(k_out), _ptr(v_out), stream or None)
 
 
 def s3_decode_attention(arena, layer, n, q, slot_off, cur_len, out, out_dtype=S3_F32, scale=0.0, stream=0):

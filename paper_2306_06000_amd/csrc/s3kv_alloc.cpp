@@ -42,20 +42,26 @@ static bool config_ok(const s3_kv_config *c) {
     if (!c) return false;
     if (c->n_layers <= 0 || c->n_heads <= 0) return false;
     if (c->head_dim != 64 && c->head_dim != 96 && c->head_dim != 128 && c->head_dim != 256) return false;
-    if (c->kv_dtype != S3_F16 && c->kv_dtype != S3_BF16 && c->kv_dtype != S3_E4M3) return false;
-    if (c->kv_dtype == S3_E4M3 && c->act_dtype != S3_F16 && c->act_dtype != S3_BF16) return false;  // 16-bit activations
+    if (c->kv_dtype != S3_F16 && c->kv_dtype != S3_BF16 && c->kv_dtype != S3_E4M3 && c->kv_dtype != S3_MXFP4) return false;
+    if ((c->kv_dtype == S3_E4M3 || c->kv_dtype == S3_MXFP4) && c->act_dtype != S3_F16 && c->act_dtype != S3_BF16) return false;  // 16-bit activations
     if (c->granule <= 0 || c->max_len <= 0 || c->max_len % c->granule != 0) return false;
     if (c->n_kv_heads < 0 || (c->n_kv_heads > 0 && (c->n_kv_heads > c->n_heads || c->n_heads % c->n_kv_heads))) return false;
     // 96-wide heads (the 64 x 96 model of the paper's table 1): multi-head 16-bit caches only
-    if (c->head_dim == 96 && (c->kv_dtype == S3_E4M3 || (c->n_kv_heads > 0 && c->n_kv_heads != c->n_heads))) return false;
+    if (c->head_dim == 96 && (c->kv_dtype == S3_E4M3 || c->kv_dtype == S3_MXFP4 || (c->n_kv_heads > 0 && c->n_kv_heads != c->n_heads))) return false;
     return true;
+}
+
+// Bytes of one cached row: H*D elements; 4-bit rows: their codes, a scale byte per 32 of them, up to a multiple of 16 bytes.
+static int64_t row_bytes_of(const s3_kv_config *cfg) {
+    const int64_t elems = (int64_t)(cfg->n_kv_heads > 0 ? cfg->n_kv_heads : cfg->n_heads) * cfg->head_dim;
+    if (cfg->kv_dtype == S3_MXFP4) return (elems / 2 + elems / 32 + 15) & ~(int64_t)15;
+    return elems * (cfg->kv_dtype == S3_E4M3 ? 1 : 2);
 }
 
 extern "C" int64_t s3_kv_bytes_per_token(const s3_kv_config *cfg) {
     if (!config_ok(cfg)) return S3_ERR_INVALID;
     // K and V, every layer, H*D two-byte numbers: 4*l*d_h bytes (section 2.1)
-    const int kv_heads = cfg->n_kv_heads > 0 ? cfg->n_kv_heads : cfg->n_heads;
-    return (int64_t)2 * cfg->n_layers * kv_heads * cfg->head_dim * (cfg->kv_dtype == S3_E4M3 ? 1 : 2);
+    return (int64_t)2 * cfg->n_layers * row_bytes_of(cfg);
 }
 
 extern "C" int s3_kv_arena_init(s3_arena **out, const s3_kv_config *cfg, void *dev_base, size_t dev_bytes) {
@@ -66,10 +72,9 @@ extern "C" int s3_kv_arena_init(s3_arena **out, const s3_kv_config *cfg, void *d
     a->cfg = *cfg;
     a->base = (char *)dev_base;
     a->dev_bytes = dev_bytes;
-    a->elem_bytes = cfg->kv_dtype == S3_E4M3 ? 1 : 2;
     if (a->cfg.n_kv_heads == 0) a->cfg.n_kv_heads = cfg->n_heads;
-    if (cfg->kv_dtype != S3_E4M3) a->cfg.act_dtype = cfg->kv_dtype;
-    a->row_bytes = (int64_t)a->cfg.n_kv_heads * cfg->head_dim * a->elem_bytes;
+    if (cfg->kv_dtype == S3_F16 || cfg->kv_dtype == S3_BF16) a->cfg.act_dtype = cfg->kv_dtype;
+    a->row_bytes = row_bytes_of(cfg);
     a->n_tokens = (int64_t)(dev_bytes / (size_t)s3_kv_bytes_per_token(cfg));
     a->plane_bytes = a->n_tokens * a->row_bytes;
     if (a->n_tokens > 0) a->free_ext[0] = a->n_tokens;
@@ -285,11 +290,13 @@ extern "C" int s3_kv_stats(const s3_arena *a, int64_t *used_tok, int64_t *free_t
 
 // The attention kernel family an arena uses depends on whether its key/value heads are shared.
 static int s3i_variants_of(const s3_arena *a) {
+    if (a->cfg.kv_dtype == S3_MXFP4) return 1;
     if (a->cfg.kv_dtype == S3_E4M3) return a->cfg.n_kv_heads < a->cfg.n_heads ? 1 : s3i_num_fp8_shapes();
     return a->cfg.n_kv_heads < a->cfg.n_heads ? s3i_num_gqa_shapes() + 1 : s3i_num_variants();  // + the matrix-core kernel
 }
 
 int s3i_kernel_kind(const s3_arena *a) {
+    if (a->cfg.kv_dtype == S3_MXFP4) return 5;
     if (a->cfg.kv_dtype == S3_E4M3) return a->cfg.n_kv_heads < a->cfg.n_heads ? 4 : 3;
     if (a->cfg.n_kv_heads >= a->cfg.n_heads) return 0;
     const int group = a->cfg.n_heads / a->cfg.n_kv_heads;

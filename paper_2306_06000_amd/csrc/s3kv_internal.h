@@ -19,8 +19,7 @@ struct s3_arena {
     char *base = nullptr;      // device memory owned by the caller (nullptr: metadata only)
     size_t dev_bytes = 0;
     int64_t n_tokens = 0;      // N: token rows the arena holds
-    int64_t elem_bytes = 2;
-    int64_t row_bytes = 0;     // kv heads * D * elem
+    int64_t row_bytes = 0;     // kv heads * D elements (4-bit rows: with their scales, up to a multiple of 16)
     int64_t plane_bytes = 0;   // N * row_bytes; plane p = 2*layer + (0: K, 1: V)
 
     std::map<int64_t, int64_t> free_ext;  // offset -> size, disjoint, coalesced
@@ -76,9 +75,11 @@ int s3i_num_fp8_shapes();  // shapes of the attention kernel for 8-bit cache row
 // Which attention kernel family the arena's next launch uses: 0 multi-head, 1 shared-K/V on the vector
 // ALU (or, with nothing set by the caller, as gqa_on_matrix_cores() says by the batch), 2 shared-K/V on the matrix cores
 // (variant index = number of shapes, or the default from four query heads per cached head; measured on MI355X), 3 the kernel for 8-bit cache rows, 4 the matrix-core
-// kernel over 8-bit rows (shared K/V heads with an 8-bit cache).
+// kernel over 8-bit rows (shared K/V heads with an 8-bit cache), 5 the kernel for rows of 4-bit blocks.
 int s3i_kernel_kind(const s3_arena *a);
 int s3i_profile_collect(s3_arena *a);  // synchronises on the recorded events and accumulates the sums
 void s3i_profile_reset(s3_arena *a);
 int s3i_device_cus(int32_t *cus);
+// Host checks of (slot_id, pos_host): every id live, 0 <= pos, pos < capacity (== capacity: S3_ERR_SLOT_FULL); nothing if either is null.
+int s3i_check_slots_host(const s3_arena *a, int32_t n, const int32_t *slot_id, const int32_t *pos_host);
 int s3i_static_scratch_setup();  // resolves the device address of the fixed scratch of s3_decode_step_static

@@ -1,8 +1,8 @@
 // Launch code of libs3kv for gfx950 (MI355X) and its small kernels: append, plane copies (grow / fill /
 // read-back), batch patches, the bandwidth probe, and the host side of every attention call.  The attention
 // kernels live in s3kv_attn.h (multi-head 16-bit caches; instantiated per head dimension by
-// s3kv_attn_inst.hip), s3kv_gqa.hip, s3kv_gqa_mfma.hip (shared key/value heads) and s3kv_fp8.hip (8-bit
-// rows) and are launched from here; the device helpers all of them share are in s3kv_device.h.
+// s3kv_attn_inst.hip), s3kv_gqa.hip, s3kv_gqa_mfma.hip (shared key/value heads), s3kv_fp8.hip (8-bit
+// rows) and s3kv_fp4.hip (rows of 4-bit blocks) and are launched from here; the device helpers all of them share are in s3kv_device.h.
 //
 // Arena layout.  Plane p = 2*layer + (0: K, 1: V) holds N token rows of H*D elements (H = cached
 // heads), token-major: element (token t, head h, d) of a plane sits at ((t*H + h)*D + d).  A slot
@@ -446,7 +446,7 @@ extern "C" void s3_kv_arena_destroy(s3_arena *a) {
 
 static bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 
-// The append of one layer: a bit copy of the new rows, or, for 8-bit caches, their quantisation.
+// The append of one layer: a bit copy of the new rows, or, for 8-bit and 4-bit caches, their quantisation.
 static int launch_append(s3_arena *a, int32_t layer, int32_t n, const int64_t *slot_off, const int32_t *pos,
                          const void *k_new, const void *v_new, void *stream) {
     if (a->cfg.kv_dtype == S3_E4M3) {
@@ -455,6 +455,12 @@ static int launch_append(s3_arena *a, int32_t layer, int32_t n, const int64_t *s
         hipLaunchKernelGGL(fn, dim3((unsigned)n, 2), dim3(256), 0, (hipStream_t)stream, a->plane(layer, 0),
                            a->plane(layer, 1), slot_off, pos, (const char *)k_new, (const char *)v_new,
                            (int32_t)a->row_bytes, a->n_tokens, a->cfg.max_len);
+    } else if (a->cfg.kv_dtype == S3_MXFP4) {
+        append_fp8_fn fn = s3i_pick_append_fp4(a->cfg.act_dtype);
+        if (!fn) return S3_ERR_INVALID;
+        hipLaunchKernelGGL(fn, dim3((unsigned)n, 2), dim3(256), 0, (hipStream_t)stream, a->plane(layer, 0),
+                           a->plane(layer, 1), slot_off, pos, (const char *)k_new, (const char *)v_new,
+                           (int32_t)(a->cfg.n_kv_heads * a->cfg.head_dim), a->n_tokens, a->cfg.max_len);
     } else {
         hipLaunchKernelGGL(append_kernel, dim3((unsigned)n, 2), dim3(256), 0, (hipStream_t)stream, a->plane(layer, 0),
                            a->plane(layer, 1), slot_off, pos, (const char *)k_new, (const char *)v_new, a->row_bytes,
@@ -463,7 +469,6 @@ static int launch_append(s3_arena *a, int32_t layer, int32_t n, const int64_t *s
     HIP_TRY(hipGetLastError());
     return S3_OK;
 }
-static int check_slots_host(const s3_arena *a, int32_t n, const int32_t *slot_id, const int32_t *pos_host);
 
 extern "C" int s3_kv_append(s3_arena *a, int32_t layer, int32_t n, const int32_t *slot_id, const int32_t *pos_host,
                             const int64_t *slot_off, const int32_t *pos, const void *k_new, const void *v_new,
@@ -471,12 +476,12 @@ extern "C" int s3_kv_append(s3_arena *a, int32_t layer, int32_t n, const int32_t
     if (!a || !a->base || layer < 0 || layer >= a->cfg.n_layers || n < 0) return S3_ERR_INVALID;
     if (n == 0) return S3_OK;
     if (!slot_off || !pos || !k_new || !v_new || !aligned16(k_new) || !aligned16(v_new)) return S3_ERR_INVALID;
-    const int rc = check_slots_host(a, n, slot_id, pos_host);
+    const int rc = s3i_check_slots_host(a, n, slot_id, pos_host);
     if (rc != S3_OK) return rc;
     return launch_append(a, layer, n, slot_off, pos, k_new, v_new, stream);
 }
 
-static int check_slots_host(const s3_arena *a, int32_t n, const int32_t *slot_id, const int32_t *pos_host) {
+int s3i_check_slots_host(const s3_arena *a, int32_t n, const int32_t *slot_id, const int32_t *pos_host) {
     if (!slot_id || !pos_host) return S3_OK;  // the caller vouches for the positions
     bool full = false;
     for (int32_t b = 0; b < n; b++) {
@@ -739,6 +744,36 @@ static size_t chunk_slots(const s3_arena *a, int n, int n_hg, size_t slot_bytes,
     return (size_t)(want > 0 && want + n > whole ? want + n : whole);
 }
 
+// Rows of 4-bit blocks: how a launch over n contexts is laid out.  A unit is what a wave's 16-byte loads cover of a row: a head
+// of 128 or 256, two neighbouring heads of 64 while their query heads fit the sixteen columns together.  A column (of the work
+// list) is a unit and up to sixteen (eight a head) of its query heads.
+struct Fp4Plan {
+    int heads_per_unit, blocks_per_head, columns, used;  // used: matrix columns that carry query heads
+    int32_t few;                                         // chunks that few contexts are cut into, 0: chunks of `chunk` rows
+    int chunk;
+    size_t slots;
+};
+static Fp4Plan fp4_plan(const s3_arena *a, int n) {
+    Fp4Plan p;
+    const int D = a->cfg.head_dim, Hkv = a->cfg.n_kv_heads, group = a->cfg.n_heads / Hkv;
+    const int64_t cus = a->num_cus > 0 ? a->num_cus : 256;
+    p.heads_per_unit = D == 64 && Hkv > 1 && group <= 8 ? 2 : 1;
+    const int width = 16 / p.heads_per_unit;
+    p.blocks_per_head = (group + width - 1) / width;
+    p.columns = (Hkv + p.heads_per_unit - 1) / p.heads_per_unit * p.blocks_per_head;
+    p.used = p.heads_per_unit * (group < width ? group : width);
+    p.chunk = a->chunk > 0 ? a->chunk : 1024;
+    const int64_t whole = (int64_t)n * ((a->cfg.max_len + p.chunk - 1) / p.chunk);
+    const int64_t fit = 2 * cus / p.columns;  // workgroups of a column that run at once
+    int64_t want = a->chunk <= 0 && n < fit ? fit : 0;
+    const size_t slot_bytes = (size_t)a->cfg.n_heads * ((size_t)D * sizeof(float) + sizeof(float2));
+    const int64_t fixed = (int64_t)((S3_STATIC_SCRATCH_BYTES - counters_bytes(p.columns)) / slot_bytes);
+    if (whole <= fixed && want > fixed - n) want = fixed - n;
+    p.few = want > 0 ? (int32_t)want : 0;
+    p.slots = (size_t)(want > 0 && want + n > whole ? want + n : whole);
+    return p;
+}
+
 // Scratch the attention calls over 1 to n sequences need at most.
 static size_t scratch_need(const s3_arena *a, int n) {
     const int D = a->cfg.head_dim, Hq = a->cfg.n_heads, kind = s3i_kernel_kind(a);
@@ -748,7 +783,9 @@ static size_t scratch_need(const s3_arena *a, int n) {
     for (int k = 1; k <= n; k++) {
         int32_t few, units;
         size_t slots;
-        if (kind != 0 && kind != 3 && gqa_on_matrix_cores(a, k)) {
+        if (kind == 5) {
+            slots = fp4_plan(a, k).slots;
+        } else if (kind != 0 && kind != 3 && gqa_on_matrix_cores(a, k)) {
             slots = gqa_partial_slots(a, k);
         } else if (kind == 0 || kind == 3) {
             slots = chunk_slots(a, k, n_hg, slot_bytes, &few, &units);
@@ -758,7 +795,8 @@ static size_t scratch_need(const s3_arena *a, int n) {
         }
         if (slots > most) most = slots;
     }
-    return counters_bytes(kind == 0 || kind == 3 ? n_hg : (int)gqa_columns(a)) + most * slot_bytes;
+    const int columns = kind == 5 ? fp4_plan(a, 1).columns : kind == 0 || kind == 3 ? n_hg : (int)gqa_columns(a);
+    return counters_bytes(columns) + most * slot_bytes;
 }
 
 extern "C" int s3_kv_reserve_scratch(s3_arena *a, int32_t max_batch) {
@@ -972,6 +1010,30 @@ static int launch_fp8(s3_arena *a, const AttnCall &c) {
     return launch_attn_kernels(a, fn, blocks, threads, dyn_lds, c.stream, args, 0, !c.static_scratch);  // the kernel merges by itself
 }
 
+// Rows of 4-bit blocks, multi-head or shared: one kernel, which in a decode step also rounds and appends the new row, merges chunks
+// and publishes the new lengths.
+static int launch_fp4(s3_arena *a, const AttnCall &c) {
+    const int D = a->cfg.head_dim;
+    const Fp4Plan p = fp4_plan(a, c.n);
+    attn_fn fn = s3i_pick_fp4(a->cfg.act_dtype, D, p.heads_per_unit, c.out_dtype == S3_F32);
+    if (!fn) return S3_ERR_INVALID;
+    AttnArgs args = common_args(a, c, a->cfg.n_kv_heads, a->cfg.n_heads, p.chunk);
+    args.few_chunks = p.few;
+    args.group = a->cfg.n_heads / a->cfg.n_kv_heads;
+    args.nqb = p.blocks_per_head;
+    args.columns = p.columns;
+    int rc = place_scratch(a, args, counters_bytes(p.columns), p.slots, c);
+    if (rc != S3_OK) return rc;
+    // LDS: the batch view, and the sums of four waves
+    const size_t pieces = 4 * (size_t)p.used * ((D == 256 ? 256 : 128) + 4) * sizeof(float);
+    while (args.ncls > 1 && batch_view_lds(c.n, args.ncls) + pieces > (size_t)144 * 1024) args.ncls--;
+    const size_t dyn_lds = ((batch_view_lds(c.n, args.ncls) + 15) & ~(size_t)15) + pieces;
+    int blocks = 0;
+    rc = stride_grid(a, (const void *)fn, 256, dyn_lds, 1, &blocks);
+    if (rc != S3_OK) return rc;
+    return launch_attn_kernels(a, fn, blocks, 256, dyn_lds, c.stream, args, 0, !c.static_scratch);  // the kernel merges by itself
+}
+
 // Mean rows of a context below which a dynamic list has one length class.  The rows decide, on the device, and not the
 // entry point.  One class against four, two layers, append + attention: 12 x 128, 300 contexts of 20..300 rows 64.3 us and
 // 59.2, 953 of 100..200 152.6 and 156.4, 953 of 2..25 48.1 and 51.5; 32 x 128, 1000 of 5..60 134.9 and 144.6; 16 x 256,
@@ -980,6 +1042,7 @@ static int launch_fp8(s3_arena *a, const AttnCall &c) {
 // Shared by s3_decode_attention and s3_decode_step (with_append: the kernel also appends and publishes the new
 // lengths).
 static int launch_attention(s3_arena *a, const AttnCall &c) {
+    if (a->cfg.kv_dtype == S3_MXFP4) return launch_fp4(a, c);
     if (a->cfg.n_kv_heads < a->cfg.n_heads) return launch_gqa(a, c);
     if (a->cfg.kv_dtype == S3_E4M3) return launch_fp8(a, c);
     const int D = a->cfg.head_dim, H = a->cfg.n_heads;
@@ -1037,7 +1100,7 @@ static int decode_step(s3_arena *a, int32_t layer, int32_t n, const int32_t *slo
     if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(out)) return S3_ERR_INVALID;
     if (len_out == pos) return S3_ERR_INVALID;  // other workgroups still read pos while len_out is written
     if (out_dtype != S3_F32 && out_dtype != S3_F16 && out_dtype != S3_BF16) return S3_ERR_INVALID;
-    const int rc = check_slots_host(a, n, slot_id, pos_host);
+    const int rc = s3i_check_slots_host(a, n, slot_id, pos_host);
     if (rc != S3_OK) return rc;
     const AttnCall c = {layer, n, q, slot_off, pos, out, out_dtype, scale, stream, true, k_new, v_new, len_out, static_scratch};
     return launch_attention(a, c);

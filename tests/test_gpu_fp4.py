@@ -1,0 +1,460 @@
+"""Rows of 4-bit blocks on the GPU, through the C ABI, against plain 64-bit forms: stored rows bit for bit, attention within the
+bound that 32-bit arithmetic has (tests/fp4_plain.py derives it)."""
+import os
+
+import numpy as np
+import pytest
+
+from paper_2306_06000_amd import binding as s3
+from tests import fp4_plain as plain
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+DEV = "cuda:0"
+TDT = {0: torch.float16, 1: torch.bfloat16, 2: torch.float32}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def need_gpu_and_lib():
+    assert torch.cuda.is_available(), "these tests need the GPU box"
+    assert os.path.exists(s3.LIB_PATH), "libs3kv.so must be built before the GPU tests run"
+    s3.lib()
+
+
+def numbers(rng, shape, act, spread=0.0):
+    """N(0,1), each head by itself times exp(U(-spread, spread)), rounded to the type: (device tensor, float64)."""
+    x = rng.standard_normal(shape) * np.exp(rng.uniform(-spread, spread, (*shape[:-1], 1)))
+    t = torch.from_numpy(x).to(TDT[act])
+    return t.to(DEV), t.double().numpy()
+
+
+class Rig:
+    """An arena with one slot a sequence, in an order other than the batch's."""
+
+    def __init__(self, heads, kv, d, act, preds, max_len=2048, granule=64, layers=1, seed=0, spare=0):
+        self.heads, self.kv, self.d, self.act = heads, kv, d, act
+        self.rng = np.random.default_rng([seed, heads, kv, d, act])
+        self.cfg = s3.make_config(layers, heads, d, s3.S3_MXFP4, granule, max_len, 0 if kv == heads else kv, act)
+        bpt = s3.s3_kv_bytes_per_token(self.cfg)
+        self.row = plain.row_bytes(kv, d)
+        caps = [s3.s3_kv_capacity_for(self.cfg, p) for p in preds]
+        self.N = sum(caps) + spare
+        self.mem = torch.full((max(self.N, 1) * bpt,), 0xA5, dtype=torch.uint8, device=DEV)
+        st, self.a = s3.s3_kv_arena_init(self.cfg, self.mem, self.mem.numel())
+        assert st == 0 and s3.s3_kv_get_param(self.a, "kernel_kind") == (0, 5)
+        order = self.rng.permutation(len(preds))
+        rc, ids, offs, _ = s3.s3_kv_alloc(self.a, [preds[i] for i in order])
+        assert rc == len(preds)
+        self.ids, self.offs = np.empty(len(preds), np.int32), np.empty(len(preds), np.int64)
+        self.ids[order], self.offs[order] = ids, offs
+        self.off_d = torch.from_numpy(self.offs).to(DEV)
+        self.stream = torch.cuda.current_stream().cuda_stream
+
+    def fill(self, lens, layer=0, spread=0.0, shift=0.0):
+        """Random rows of every sequence, as they are stored; keeps their numbers."""
+        self.k, self.v = [], []
+        for sid, L in zip(self.ids.tolist(), lens):
+            rows = [plain.to_rows(numbers(self.rng, (L, self.kv, self.d), self.act, spread)[1] + shift, self.act) for _ in range(2)]
+            if L:
+                kd, vd = (torch.from_numpy(r).to(DEV) for r in rows)
+                assert s3.s3_kv_fill(self.a, sid, layer, 0, L, kd, vd, self.stream) == 0
+            self.k.append(plain.from_rows(rows[0], self.kv, self.d))
+            self.v.append(plain.from_rows(rows[1], self.kv, self.d))
+
+    def read(self, i, which, rows, layer=0):
+        dst = torch.empty((rows, self.row), dtype=torch.uint8, device=DEV)
+        assert s3.s3_kv_read_rows(self.a, int(self.ids[i]), layer, which, 0, rows, dst, self.stream) == 0
+        return dst.cpu().numpy()
+
+    def lens_d(self, lens):
+        return torch.tensor(lens, dtype=torch.int32, device=DEV)
+
+    def attend(self, q, lens, out_dtype=s3.S3_F32, scale=0.0, layer=0, off=None):
+        out = torch.full((len(lens), self.heads, self.d), float("nan"), dtype=TDT[out_dtype], device=DEV)
+        off = self.off_d if off is None else off
+        assert s3.s3_decode_attention(self.a, layer, len(lens), q, off, self.lens_d(lens), out, out_dtype, scale, self.stream) == 0
+        torch.cuda.synchronize()
+        return out
+
+    def check(self, out, q64, lens, out_dtype, scale=None, what=""):
+        got = out.double().cpu().numpy()
+        for b, L in enumerate(lens):
+            want, bound = plain.attention(q64[b], self.k[b][:L], self.v[b][:L], scale)
+            parts = np.abs(self.v[b][:L]).max(0).repeat(self.heads // self.kv, 0) if L else np.zeros_like(want)
+            tol = plain.allowed(want, bound, parts, out_dtype)
+            off = np.abs(got[b] - want)
+            assert (off <= tol).all(), (what, b, L, float((off / tol).max()), float(off.max()))
+
+    def close(self):
+        torch.cuda.synchronize()
+        s3.s3_kv_arena_destroy(self.a)
+
+
+SHAPES = [(16, 16, 256), (12, 12, 128), (3, 3, 128), (16, 16, 64), (7, 7, 64), (32, 8, 128), (16, 1, 256), (8, 1, 64), (24, 8, 64), (40, 5, 128),
+          (6, 3, 256), (20, 1, 128), (36, 2, 64), (20, 2, 64), (40, 1, 64), (34, 2, 256), (9, 3, 64), (64, 2, 128)]
+
+
+@pytest.mark.parametrize("act", [0, 1], ids=["f16", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "%dq%dkv%d" % s)
+def test_attention_over_shapes_and_lengths(shape, act):
+    lens = [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 129, 257, 500]
+    rig = Rig(*shape, act, [max(L, 1) for L in lens])
+    rig.fill(lens, spread=1.0)
+    q, q64 = numbers(rig.rng, (len(lens), rig.heads, rig.d), act, 0.5)
+    for out_dtype in (2, act):
+        out = rig.attend(q, lens, out_dtype)
+        rig.check(out, q64, lens, out_dtype, what=shape)
+        assert (out[0] == 0).all()
+    rig.close()
+
+
+@pytest.mark.parametrize("shape,n,longest", [((32, 8, 128), 3, 7001), ((16, 16, 256), 1, 3333), ((16, 1, 256), 2, 9000), ((24, 8, 64), 5, 2047),
+                                             ((3, 3, 128), 40, 1500), ((12, 12, 128), 300, 90), ((8, 1, 64), 700, 60), ((32, 8, 128), 130, 400)],
+                         ids=str)
+def test_attention_over_batches(shape, n, longest):
+    rng = np.random.default_rng(n)
+    lens = rng.integers(1, longest + 1, n).tolist()
+    lens[0] = longest
+    rig = Rig(*shape, 1, lens, max_len=16384)
+    rig.fill(lens)
+    q, q64 = numbers(rig.rng, (n, rig.heads, rig.d), 1)
+    rig.check(rig.attend(q, lens), q64, lens, 2, what=(shape, n))
+    first = rig.attend(q, lens)
+    for _ in range(3):  # the order in which chunks meet does not show
+        assert torch.equal(first, rig.attend(q, lens))
+    rig.close()
+
+
+def test_chunks_grids_classes_and_both_orderings():
+    lens = [0, 1, 33, 700, 1999, 64, 350, 1]
+    rig = Rig(32, 8, 128, 1, [max(L, 1) for L in lens])
+    rig.fill(lens)
+    q, q64 = numbers(rig.rng, (len(lens), 32, 128), 1)
+    for chunk in (32, 96, 512, 2048, 0):
+        for grid in (1, 7, 100, 3000, 0):
+            for sync, classes in ((0, 0), (1, 3)):
+                for name, value in (("chunk", chunk), ("grid_blocks", grid), ("merge_sync", sync), ("classes", classes)):
+                    assert s3.s3_kv_set_param(rig.a, name, value) == 0
+                rig.check(rig.attend(q, lens), q64, lens, 2, what=(chunk, grid, sync))
+    rig.close()
+
+
+@pytest.mark.parametrize("scale", [1e-3, 0.3, 2.0])
+def test_scale_and_scores_that_spread(scale):
+    """Large scores: the weights collapse onto few rows; the maximum comes early, late and in the middle."""
+    lens = [400, 401, 90, 64]
+    rig = Rig(8, 2, 128, 0, lens)
+    rig.fill(lens, spread=0.5)
+    q, q64 = numbers(rig.rng, (4, 8, 128), 0)
+    rig.check(rig.attend(q, lens, 2, scale), q64, lens, 2, float(np.float32(scale)), what=scale)
+    rig.close()
+
+
+@pytest.mark.parametrize("act", [0, 1], ids=["f16", "bf16"])
+@pytest.mark.parametrize("heads,d", [(16, 256), (8, 128), (3, 128), (5, 64), (16, 64), (1, 64)])
+def test_append_rounds_bit_exactly_and_fetch_reads_back(act, heads, d):
+    n = 24
+    rig = Rig(heads, heads, d, act, [8] * n, layers=2)
+    x, x64 = [], []
+    for _ in range(2):
+        t = torch.from_numpy(rig.rng.standard_normal((n, heads, d)) * np.exp(rig.rng.uniform(-9, 9, (n, heads, 1)))).to(TDT[act])
+        t[1] = 0
+        t[2] = -0.0
+        t[3] = torch.tensor([1, 0.5, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5, 6, 6.5, 6.984375, -5, -0.25, -1.75, 3], dtype=TDT[act]).repeat(d // 16)
+        t[4] = t[3] * 2 ** -9
+        t[5] = 7.0
+        t[6] = torch.finfo(TDT[act]).max
+        t[7] = torch.finfo(TDT[act]).tiny * 0.25  # below the normal numbers
+        t[8, 0, 5] = float("nan")
+        t[9, heads - 1, d - 1] = float("inf")
+        t[10, 0, 31] = -float("inf")
+        t[11] = -torch.finfo(TDT[act]).max * 0.9
+        x.append(t.to(DEV))
+        x64.append(t.double().numpy())
+    pos = torch.arange(n, dtype=torch.int32, device=DEV) % 5
+    before = rig.mem.clone()
+    assert s3.s3_kv_append(rig.a, 1, n, rig.off_d, pos, x[0], x[1], rig.stream) == 0
+    got = rig.mem.view(2, 2, rig.N, rig.row).cpu().numpy()
+    old = before.view(2, 2, rig.N, rig.row).cpu().numpy()
+    at = rig.offs + pos.cpu().numpy()
+    for which in range(2):
+        want = old[1, which].copy()
+        want[at] = plain.to_rows(x64[which], act)
+        assert np.array_equal(got[1, which], want)
+    assert np.array_equal(got[0], old[0])
+    k, v = [torch.full((n, heads, d), 77.0, dtype=TDT[act], device=DEV) for _ in range(2)]
+    assert s3.s3_kv_fetch(rig.a, 1, n, rig.off_d, pos, k, v, rig.stream) == 0
+    for which, t in ((0, k), (1, v)):
+        want = plain.from_rows(got[1, which][at], heads, d)
+        assert np.array_equal(t.double().cpu().numpy(), want, equal_nan=True)
+        finite = np.isfinite(x64[which].reshape(n, -1, 32)).all(-1)
+        assert np.array_equal(np.isfinite(t.double().cpu().numpy().reshape(n, -1, 32)).all(-1), finite)
+    only = torch.full_like(k, 5.0)  # one of the two, and entries that are refused
+    off = rig.off_d.clone()
+    off[3], off[5] = -1, rig.N
+    bad = pos.clone()
+    bad[7], bad[8] = -1, 2048
+    assert s3.s3_kv_fetch(rig.a, 1, n, off, bad, None, only, rig.stream) == 0
+    skip = torch.tensor([3, 5, 7, 8], device=DEV)
+    assert (only[skip] == 5).all() and torch.equal(only[9:].nan_to_num(3.0), v[9:].nan_to_num(3.0))
+    rig.close()
+
+
+def test_every_code_under_scales_over_the_whole_range():
+    """Filled rows may hold any scale byte; a context of one row returns its values."""
+    rig = Rig(4, 4, 64, 1, [1] * 64)
+    codes = np.arange(4 * 32, dtype=np.uint8).reshape(1, -1).repeat(64, 0) + (np.arange(64, dtype=np.uint8)[:, None] % 2) * 128
+    rows = np.zeros((64, rig.row), np.uint8)
+    rows[:, :128] = codes
+    scales = np.array([1, 2, 60, 100, 126, 127, 128, 150, 200, 252, 255, 90, 110, 120, 130, 140], np.uint8)
+    rows[:, 128:136] = scales[(np.arange(64)[:, None] + np.arange(8)) % 16]
+    kd = torch.zeros((1, rig.row), dtype=torch.uint8, device=DEV)
+    for i in range(64):
+        assert s3.s3_kv_fill(rig.a, int(rig.ids[i]), 0, 0, 1, kd, torch.from_numpy(rows[i:i + 1].copy()).to(DEV), rig.stream) == 0
+    q, _ = numbers(rig.rng, (64, 4, 64), 1)
+    got = rig.attend(q, [1] * 64).double().cpu().numpy()
+    want = plain.from_rows(rows, 4, 64)
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    fine = ~np.isnan(want)
+    assert np.allclose(got[fine], want[fine], rtol=2.0 ** -22, atol=2.0 ** -125)  # 1/sum and the product with it
+    rig.close()
+
+
+@pytest.mark.parametrize("shape,act", [((16, 16, 256), 0), ((32, 8, 128), 1), ((16, 1, 256), 1), ((24, 8, 64), 0), ((5, 5, 64), 1), ((8, 1, 64), 0),
+                                       ((20, 1, 128), 1), ((36, 2, 64), 1), ((40, 1, 128), 0)], ids=str)
+@pytest.mark.parametrize("chunk", [0, 64])
+def test_step_is_append_and_attention(shape, act, chunk):
+    """Bit for bit, outputs and stored rows, a row at every place of a tile; the new lengths; nothing else of the arena."""
+    pos = [0, 1, 14, 15, 16, 30, 31, 32, 33, 62, 63, 64, 65, 95, 127, 128, 300, 511, 1023]
+    n = len(pos)
+    one, two = (Rig(*shape, act, [p + 1 for p in pos], seed=3) for _ in range(2))
+    outs = []
+    for rig in (one, two):
+        assert s3.s3_kv_set_param(rig.a, "chunk", chunk) == 0
+        rig.fill(pos)
+    rng = np.random.default_rng(9)
+    (q, q64), (k, k64), (v, v64) = (numbers(rng, (n, h, one.d), act, 1.0) for h in (one.heads, one.kv, one.kv))
+    for rig in (one, two):
+        out = torch.full((n, rig.heads, rig.d), float("nan"), dtype=torch.float32, device=DEV)
+        new = torch.full((n,), -7, dtype=torch.int32, device=DEV)
+        p = rig.lens_d(pos)
+        if rig is one:
+            assert s3.s3_decode_step(rig.a, 0, n, rig.off_d, p, q, k, v, out, 2, 0.0, new, rig.stream, slot_id=rig.ids, pos_host=pos) == 0
+            torch.cuda.synchronize()
+            assert new.tolist() == [x + 1 for x in pos]
+        else:
+            assert s3.s3_kv_append(rig.a, 0, n, rig.off_d, p, k, v, rig.stream) == 0
+            out = rig.attend(q, [x + 1 for x in pos])
+        outs.append(out)
+    assert torch.equal(one.mem, two.mem)
+    assert torch.equal(outs[0], outs[1])
+    for i in range(n):
+        one.k[i] = np.concatenate([one.k[i], plain.from_rows(plain.to_rows(k64[i:i + 1], act), one.kv, one.d)])
+        one.v[i] = np.concatenate([one.v[i], plain.from_rows(plain.to_rows(v64[i:i + 1], act), one.kv, one.d)])
+    one.check(outs[0], q64, [x + 1 for x in pos], 2)
+    one.close()
+    two.close()
+
+
+def test_step_checks_and_refused_entries():
+    rig = Rig(8, 2, 128, 1, [64, 64, 64, 64], spare=64)
+    rig.fill([64, 10, 20, 30])
+    n = 4
+    (q, _), (k, _), (v, _) = (numbers(rig.rng, (n, h, 128), 1) for h in (8, 2, 2))
+    out = torch.full((n, 8, 128), float("nan"), dtype=torch.float32, device=DEV)
+    args = (rig.a, 0, n, rig.off_d, rig.lens_d([64, 10, 20, 30]), q, k, v, out)
+    before = rig.mem.clone()
+    assert s3.s3_decode_step(*args, slot_id=rig.ids, pos_host=[64, 10, 20, 30]) == s3.S3_ERR_SLOT_FULL
+    assert s3.s3_decode_step(*args, slot_id=rig.ids, pos_host=[65, 10, 20, 30]) == s3.S3_ERR_INVALID
+    assert s3.s3_decode_step(*args[:4], rig.lens_d([1] * 4), q, k, v, out, out_dtype=s3.S3_MXFP4) == s3.S3_ERR_INVALID
+    pos = rig.lens_d([5, -1, 2048, 30])
+    off = rig.off_d.clone()
+    off[0] = -1
+    new = torch.zeros(4, dtype=torch.int32, device=DEV)
+    torch.cuda.synchronize()
+    assert torch.equal(rig.mem, before)
+    assert s3.s3_decode_step(rig.a, 0, n, off, pos, q, k, v, out, 2, 0.0, new, rig.stream) == 0
+    torch.cuda.synchronize()
+    assert (out[:3] == 0).all() and torch.isfinite(out[3]).all() and out[3].abs().sum() > 0
+    changed = (rig.mem != before).view(2, rig.N, rig.row).any(-1)
+    assert changed.nonzero()[:, 1].unique().tolist() == [int(rig.offs[3]) + 30]
+    rig.close()
+
+
+@pytest.mark.parametrize("shape", [(4, 4, 64), (8, 2, 64), (6, 3, 64), (4, 4, 128)], ids=str)
+def test_a_block_that_is_nan_stays_with_its_head(shape):
+    """A key block: its head's queries; a value block: its 32 elements; other heads and other sequences keep their numbers."""
+    heads, kv, d = shape
+    rig = Rig(*shape, 1, [70, 70, 70])
+    rig.fill([70] * 3)
+    q, q64 = numbers(rig.rng, (3, heads, d), 1)
+    clean = rig.attend(q, [70] * 3)
+    group, head = heads // kv, kv - 1 if kv % 2 == 0 else 1
+    for which in range(2):
+        for row in (3, 40, 69):
+            rig.fill([70] * 3)
+            for i in range(3):
+                rows = [plain.to_rows(x, 1) for x in (rig.k[i], rig.v[i])]
+                kd, vd = (torch.from_numpy(r).to(DEV) for r in rows)
+                assert s3.s3_kv_fill(rig.a, int(rig.ids[i]), 0, 0, 70, kd, vd, rig.stream) == 0
+            clean = rig.attend(q, [70] * 3)
+            rows = [plain.to_rows(x, 1) for x in (rig.k[1], rig.v[1])]
+            rows[which][row, kv * d // 2 + head * (d // 32)] = 255
+            kd, vd = (torch.from_numpy(r).to(DEV) for r in rows)
+            assert s3.s3_kv_fill(rig.a, int(rig.ids[1]), 0, 0, 70, kd, vd, rig.stream) == 0
+            got = rig.attend(q, [70] * 3)
+            bad = torch.zeros_like(got, dtype=torch.bool)
+            bad[1, head * group:(head + 1) * group, :d if which == 0 else 32] = True
+            assert torch.isnan(got[bad]).all() and torch.equal(got[~bad], clean[~bad]), (which, row)
+    rig.close()
+
+
+def test_queries_that_are_not_finite_and_equal_scores():
+    rig = Rig(8, 2, 128, 0, [100, 100, 33])
+    rig.fill([100, 100, 33])
+    q, q64 = numbers(rig.rng, (3, 8, 128), 0)
+    clean = rig.attend(q, [100, 100, 33])
+    bad = q.clone()
+    bad[0, 3, 7], bad[1, 5, 0] = float("nan"), float("inf")
+    got = rig.attend(bad, [100, 100, 33])
+    assert torch.isnan(got[0, 3]).all() and torch.isnan(got[1, 5]).all()
+    keep = torch.ones(3, 8, dtype=torch.bool, device=DEV)
+    keep[0, 3] = keep[1, 5] = False
+    assert torch.equal(got[keep], clean[keep])
+    got = rig.attend(torch.zeros_like(q), [100, 100, 33]).double().cpu().numpy()
+    for b, L in enumerate([100, 100, 33]):
+        want = rig.v[b][:L].mean(0).repeat(4, 0)
+        assert np.abs(got[b] - want).max() <= (L + 8) * 2.0 ** -24 * np.abs(rig.v[b]).max()
+    rig.close()
+
+
+def test_rows_move_as_they_are():
+    """Doubling, compaction, eviction, staged eviction: stored bytes, and the attention after them."""
+    lens = [64, 30, 50]
+    rig = Rig(8, 2, 64, 1, [64, 64, 64], layers=2, spare=320)
+    rig.fill(lens)
+    want = [[rig.read(i, w, lens[i]) for w in range(2)] for i in range(3)]
+    q, q64 = numbers(rig.rng, (3, 8, 64), 1)
+    st, off, cap = s3.s3_kv_grow(rig.a, int(rig.ids[0]), 64, rig.stream)
+    assert st == 0 and cap == 128
+    assert s3.s3_kv_gather_rows(rig.a, int(rig.ids[1]), 30, stage := torch.zeros(s3.s3_kv_evict_bytes(rig.a, 30), dtype=torch.uint8, device=DEV), rig.stream) == 0
+    host = torch.zeros(s3.s3_kv_evict_bytes(rig.a, 50), dtype=torch.uint8).pin_memory()
+    assert s3.s3_kv_evict(rig.a, int(rig.ids[2]), 50, host, rig.stream) == 0
+    torch.cuda.synchronize()
+    st, sid, off2, _ = s3.s3_kv_restore(rig.a, 128, 50, host, rig.stream)
+    assert st == 0
+    rig.ids[2] = sid
+    assert s3.s3_kv_free(rig.a, int(rig.ids[1])) == 0
+    rc, ids, offs, _ = s3.s3_kv_alloc(rig.a, [40])
+    assert rc == 1 and s3.s3_kv_scatter_rows(rig.a, int(ids[0]), 30, stage, rig.stream) == 0
+    rig.ids[1] = ids[0]
+    st, new_off, _ = s3.s3_kv_compact(rig.a, rig.ids, lens, rig.stream)
+    assert st == 0
+    for i in range(3):
+        for w in range(2):
+            assert np.array_equal(rig.read(i, w, lens[i]), want[i][w])
+    rig.check(rig.attend(q, lens, off=torch.from_numpy(new_off).to(DEV)), q64, lens, 2)
+    rig.close()
+
+
+def test_static_step_and_replayed_graphs():
+    """The step without allocations, recorded and replayed between eager work of other batches, against the eager step."""
+    shape, n = (32, 8, 128), 5
+    pos = [1900, 3, 700, 63, 1023]
+    rig = Rig(*shape, 1, [p + 1 for p in pos])
+    rig.fill(pos)
+    (q, _), (k, _), (v, _) = (numbers(rig.rng, (n, h, 128), 1) for h in (32, 8, 8))
+    p = rig.lens_d(pos)
+    outs = [torch.full((n, 32, 128), float("nan"), dtype=torch.bfloat16, device=DEV) for _ in range(4)]
+    assert s3.s3_decode_step(rig.a, 0, n, rig.off_d, p, q, k, v, outs[0], 1, 0.0, None, rig.stream) == 0
+    assert s3.s3_decode_step_static(rig.a, 0, n, rig.off_d, p, q, k, v, outs[1], 1, 0.0, None, rig.stream) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[1])
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        graphs = []
+        for fn, out in ((s3.s3_decode_step, outs[2]), (s3.s3_decode_step_static, outs[3])):
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=side):
+                assert fn(rig.a, 0, n, rig.off_d, p, q, k, v, out, 1, 0.0, None, side.cuda_stream) == 0
+            graphs.append(g)
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for g, out in zip(graphs, outs[2:]):
+            out.fill_(float("nan"))
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, outs[0])
+        assert torch.equal(rig.attend(q, [x + 1 for x in pos], 1), outs[0])
+    rig.close()
+
+
+def test_static_step_that_needs_more_than_the_fixed_scratch():
+    rig = Rig(64, 64, 256, 1, [1] * 200, max_len=16384)
+    n = 200
+    q = torch.zeros((n, 64, 256), dtype=torch.bfloat16, device=DEV)
+    out = torch.zeros_like(q)
+    assert s3.s3_decode_step_static(rig.a, 0, n, rig.off_d, rig.lens_d([0] * n), q, q, q, out, 1) == s3.S3_ERR_SCRATCH
+    assert s3.s3_decode_step(rig.a, 0, n, rig.off_d, rig.lens_d([0] * n), q, q, q, out, 1) == 0
+    rig.close()
+
+
+def test_other_streams_and_layers():
+    lens = [200, 31, 77]
+    rig = Rig(16, 4, 64, 1, lens, layers=3)
+    q, q64 = numbers(rig.rng, (3, 16, 64), 1)
+    side = torch.cuda.Stream()
+    rig.stream = side.cuda_stream
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for layer in (2, 0, 1):
+            rig.fill(lens, layer=layer)
+            rig.check(rig.attend(q, lens, layer=layer), q64, lens, 2)
+    rig.close()
+
+
+def test_largest_batch():
+    n = 4095
+    rng = np.random.default_rng(4)
+    lens = rng.integers(0, 40, n).tolist()
+    rig = Rig(2, 1, 64, 1, [max(L, 1) for L in lens])
+    rig.fill(lens)
+    q, q64 = numbers(rig.rng, (n, 2, 64), 1)
+    rig.check(rig.attend(q, lens), q64, lens, 2)
+    extra = torch.zeros((n + 1, 2, 64), dtype=torch.bfloat16, device=DEV)
+    assert s3.s3_decode_attention(rig.a, 0, n + 1, extra, rig.off_d, rig.lens_d(lens), extra, 1) == s3.S3_ERR_INVALID
+    rig.close()
+
+
+def test_rows_far_into_a_plane():
+    """A slot more than 4 GiB into its plane: append, step, fetch, read-back."""
+    heads, d = 32, 256  # 4352 bytes a row
+    cfg = s3.make_config(1, heads, d, s3.S3_MXFP4, 64, 1 << 20, 0, 1)
+    row = plain.row_bytes(heads, d)
+    rows = (1 << 20) + 256
+    mem = torch.empty(2 * rows * row, dtype=torch.uint8, device=DEV)
+    st, a = s3.s3_kv_arena_init(cfg, mem, mem.numel())
+    assert st == 0
+    rc, ids, offs, _ = s3.s3_kv_alloc(a, [1 << 20, 128])
+    assert rc == 2 and int(offs[1]) * row > 1 << 32
+    rng = np.random.default_rng(1)
+    (k, k64), (v, v64), (q, q64) = (numbers(rng, (70, heads, d), 1) for _ in range(3))
+    off = torch.full((70,), int(offs[1]), dtype=torch.int64, device=DEV)
+    pos = torch.arange(70, dtype=torch.int32, device=DEV)
+    assert s3.s3_kv_append(a, 0, 69, off, pos, k, v) == 0
+    out = torch.zeros((1, heads, d), dtype=torch.float32, device=DEV)
+    assert s3.s3_decode_step(a, 0, 1, off[69:], pos[69:], q[69:], k[69:], v[69:], out) == 0
+    back = torch.zeros_like(k)
+    assert s3.s3_kv_fetch(a, 0, 70, off, pos, back, None) == 0
+    kk, vv = (plain.from_rows(plain.to_rows(x, 1), heads, d) for x in (k64, v64))
+    assert np.array_equal(back.double().cpu().numpy(), kk)
+    want, bound = plain.attention(q64[69], kk, vv)
+    assert (np.abs(out[0].double().cpu().numpy() - want) <= plain.allowed(want, bound, np.abs(vv).max(0), 2)).all()
+    # and a context whose rows span more than 4 GiB of a plane, at its far end
+    far = torch.tensor([(1 << 20) - 1], dtype=torch.int32, device=DEV)
+    assert s3.s3_decode_step(a, 0, 1, torch.zeros(1, dtype=torch.int64, device=DEV), far, q[:1], k[:1], v[:1], out) == 0
+    got = torch.empty((1, row), dtype=torch.uint8, device=DEV)
+    assert s3.s3_kv_read_rows(a, int(ids[0]), 0, 0, (1 << 20) - 1, 1, got) == 0
+    assert np.array_equal(got.cpu().numpy(), plain.to_rows(k64[:1], 1))
+    torch.cuda.synchronize()
+    s3.s3_kv_arena_destroy(a)
