@@ -205,7 +205,7 @@ typedef struct {
     float eps;            /* of the norms, >= 0                                                                    */
     const float *inv_freq;         /* DEVICE [rotary_dim/2] radians per position                                   */
     const uint8_t *axis_of_pair;   /* HOST [rotary_dim/2], each < n_axes; NULL with one axis                       */
-    const float *q_weight, *k_weight; /* DEVICE [head_dim] or NULL: that norm is left out                          */
+    const float *q_weight, *k_weight; /* DEVICE [head_dim], 16-byte aligned, or NULL: that norm is left out        */
 } s3_rotary;
 
 /* Norms and rotation of n tokens' queries and keys, in one pass, without a cache.

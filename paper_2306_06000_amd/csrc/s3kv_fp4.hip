@@ -54,46 +54,38 @@ struct Fp4Tile {
     unsigned vs[8];
 };
 
-template <int D, int NH>
-struct Fp4Lane {  // byte offsets of a lane within a row
-    int k, ks, v, vs;
+// Where a lane's pieces of a tile are, in bytes from its first row.
+struct Fp4Offsets {
+    unsigned k[2], ks[2], v[8], vs[8];
 };
 
-template <int W>
-__device__ __forceinline__ unsigned load_v_words(const char *p, unsigned (&v)[W / 128]) {
-    if constexpr (W == 256) {
-        const u32x2 w = __builtin_nontemporal_load((const u32x2 *)p);
-        v[0] = w[0];
-        v[1] = w[1];
-    } else {
-        v[0] = __builtin_nontemporal_load((const unsigned *)p);
-    }
-    return 0;
+// Rows of one plane from `base` on, `rows` of them; what lies past them reads as zeros and costs no traffic (a scale of 0 under codes
+// of 0: no NaN comes from there).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(const char *base, int rows, int row_bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, max(rows, 0) * row_bytes, 0x00020000);
 }
 
-// rows: how many rows of the tile there are (32 but for the last tile: rows past the end read the last one again).
-template <int W, bool FULL>
-__device__ __forceinline__ void load_tile(Fp4Tile<W> &t, const char *kbase, const char *vbase, int row_bytes, int rows, int ko, int kso, int vo,
-                                          int vso) {
+template <int W>
+__device__ __forceinline__ void load_tile(Fp4Tile<W> &t, const char *kbase, const char *vbase, int rows, int row_bytes, const Fp4Offsets &o) {
     constexpr int T = W / 128;
-    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const __amdgpu_buffer_rsrc_t kr = rows_from(kbase, rows, row_bytes), vr = rows_from(vbase, rows, row_bytes);
 #pragma unroll
-    for (int u = 0; u < 2; u++) {
-        const int row = FULL ? 16 * u + r : min(16 * u + r, rows - 1);
-        const unsigned at = (unsigned)(row * row_bytes);
+    for (int u = 0; u < 2; u++)
 #pragma unroll
         for (int h = 0; h < T; h++) {
-            t.k[u][h] = __builtin_nontemporal_load((const u32x4 *)(kbase + at + ko + 64 * h));
-            t.ks[u][h] = *(const unsigned char *)(kbase + at + kso + 4 * h);
+            t.k[u][h] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kr, o.k[u] + 64 * h, 0, 2));
+            t.ks[u][h] = __builtin_amdgcn_raw_buffer_load_b8(kr, o.ks[u] + 4 * h, 0, 0);
         }
-    }
 #pragma unroll
     for (int e = 0; e < 8; e++) {
-        const int want = (e & 3) + 4 * g + 16 * (e >> 2);
-        const int row = FULL ? want : min(want, rows - 1);
-        const unsigned at = (unsigned)(row * row_bytes);
-        load_v_words<W>(vbase + at + vo, t.v[e]);
-        t.vs[e] = *(const unsigned char *)(vbase + at + vso);
+        if constexpr (W == 256) {
+            const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(vr, o.v[e], 0, 2));
+            t.v[e][0] = w[0];
+            t.v[e][1] = w[1];
+        } else {
+            t.v[e][0] = __builtin_amdgcn_raw_buffer_load_b32(vr, o.v[e], 0, 2);
+        }
+        t.vs[e] = __builtin_amdgcn_raw_buffer_load_b8(vr, o.vs[e], 0, 0);
     }
 }
 
@@ -136,21 +128,284 @@ __device__ __forceinline__ void widen_pairs(const unsigned (&v)[8], const float 
     hi = pack_words(h[0], h[1], h[2], h[3]);
 }
 
-// NH: heads of a unit (2 only for D = 64); QP: bf16 parts of a query; NP: bf16 parts of a weight.
+// What one wave does with the rows of a unit.  NH: heads of a unit (2 only for D = 64); NP: bf16 parts of a weight.
 template <int ACT, int D, int NH, int NP>
-__global__ void __launch_bounds__(256, 2) attn_fp4_kernel(const AttnArgs a) {
-    constexpr int W = D == 256 ? 256 : 128, T = W / 128, TS = 4;
-    constexpr int QP = ACT == S3_F16 ? 2 : 1;
-    constexpr int QB = 16 / NH;              // columns of a head
-    constexpr int STRIDE = W + 4;            // floats of a column in LDS
-    extern __shared__ __align__(16) char dyn_lds[];  // the batch view, then the waves' sums of the columns in use
-    __shared__ int wave_sums[S3_MAX_CLASSES * S3_MAX_WAVES];
-    __shared__ float comb_m[TS][16], comb_l[TS][16];
-    __shared__ int last_of_context;
-    const int lane = threadIdx.x & 63, ts = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-    const BatchView bv = build_batch_view<false>(a, dyn_lds, wave_sums);
-    float *comb = (float *)(dyn_lds + ((batch_view_bytes(a.n, a.ncls) + 15) & ~(size_t)15));
-    // the new lengths, and a zero output row for empty or refused contexts, by the workgroups in turn
+struct Fp4Wave {
+    static constexpr int W = D == 256 ? 256 : 128, T = W / 128;
+    static constexpr int QP = ACT == S3_F16 ? 2 : 1;  // bf16 parts of a query
+    static constexpr int QB = 16 / NH;                // columns of a head
+    static constexpr int Q_BYTES = QP * T * 4 * 1024;  // of the queries in LDS
+
+    const AttnArgs &a;
+    char *q_lds;  // the queries, as the B operand takes them: [part][half][word][lane]
+    int lane, r, g;
+    int code_bytes, row_bytes;
+    int kh0, qb, per_head;  // first cached head, block of query heads, query heads of a cached head in it
+    bool second;            // the unit has two heads
+    int ksub, vsub, qsub, kblk, vel, khead, vhead, qhead;
+    int ko, kso, vo, vso;
+    bool column, q_here;
+    Fp4Offsets at_row;
+    float m, l;
+    f32x4 acc[8 * T];
+
+    __device__ __forceinline__ Fp4Wave(const AttnArgs &args, char *lds) : a(args), q_lds(lds) {
+        lane = threadIdx.x & 63;
+        r = lane & 15;
+        g = lane >> 4;
+        code_bytes = fp4_code_bytes(a.H, D);
+        row_bytes = fp4_row_bytes(a.H, D);
+    }
+
+    // Which heads: of the A operand's lanes (K: block group g; V: elements of lane m = r), of the B operand's columns.
+    __device__ __forceinline__ void set_column(int col) {
+        const int unit = a.nqb == 1 ? col : col / a.nqb;
+        qb = col - unit * a.nqb;
+        kh0 = unit * NH;
+        second = NH == 2 && kh0 + 1 < a.H;
+        per_head = min(a.group - qb * QB, QB);
+        ksub = NH == 2 ? g >> 1 : 0;
+        vsub = qsub = NH == 2 ? r >> 3 : 0;
+        khead = kh0 + (second ? ksub : 0);
+        vhead = kh0 + (second ? vsub : 0);
+        kblk = D == 64 ? g & 1 : g;                             // (+ 4 for the second half of 256)
+        vel = D == 256 ? 16 * r : D == 64 ? 8 * (r & 7) : 8 * r;  // first element of the V words
+        ko = khead * (D / 2) + kblk * 16;
+        kso = code_bytes + khead * (D / 32) + kblk;
+        vo = vhead * (D / 2) + vel / 2;
+        vso = code_bytes + vhead * (D / 32) + vel / 32;
+        const int qi = (r % QB) + qb * QB;
+        qhead = (kh0 + qsub) * a.group + qi;
+        column = qi < a.group && (NH == 1 || qsub == 0 || second);
+        q_here = column && (D != 64 || (NH == 2 ? ksub == qsub : g < 2));
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+            at_row.k[u] = (16 * u + r) * row_bytes + ko;
+            at_row.ks[u] = (16 * u + r) * row_bytes + kso;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            const int row = (e & 3) + 4 * g + 16 * (e >> 2);
+            at_row.v[e] = row * row_bytes + vo;
+            at_row.vs[e] = row * row_bytes + vso;
+        }
+    }
+
+    // Sequence b's queries into LDS (fp16: two exact bf16 parts); nothing folded in yet.
+    __device__ __forceinline__ void begin(int b) {
+        u32x4 w[T][4];
+#pragma unroll
+        for (int h = 0; h < T; h++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                w[h][i] = (u32x4){0u, 0u, 0u, 0u};
+                if (q_here) w[h][i] = *(const u32x4 *)(a.q + (((int64_t)b * a.Hq + qhead) * D + h * 128 + kblk * 32 + i * 8) * 2);
+            }
+#pragma unroll
+        for (int h = 0; h < T; h++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                if (QP == 1) {
+                    put_query(0, h, i, w[h][i]);
+                } else {
+                    float x[8];
+                    widen8<ACT>(w[h][i], x);
+#pragma unroll
+                    for (int part = 0; part < QP; part++) {
+                        u32x4 p;
+#pragma unroll
+                        for (int e = 0; e < 4; e++) p[e] = take_bf16_part(x[2 * e], x[2 * e + 1]);
+                        put_query(part, h, i, p);
+                    }
+                }
+            }
+        m = -INFINITY;
+        l = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8 * T; i++) acc[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+    __device__ __forceinline__ void put_query(int part, int h, int i, const u32x4 w) {
+        *(u32x4 *)(q_lds + (((part * T + h) * 4 + i) * 64 + lane) * 16) = w;
+    }
+    __device__ __forceinline__ bf16x8 query(int part, int h, int i) const {
+        return __builtin_bit_cast(bf16x8, *(const u32x4 *)(q_lds + (((part * T + h) * 4 + i) * 64 + lane) * 16));
+    }
+
+    __device__ __forceinline__ void load(Fp4Tile<W> &t, const char *kp, const char *vp, int rows) const {
+        load_tile<W>(t, kp, vp, rows, row_bytes, at_row);
+    }
+
+    // What a tile holds is folded into (m, l, acc); rows: those of the tile and behind it (fewer than 32: the last tile).
+    __device__ __forceinline__ void fold(const Fp4Tile<W> &t, int rows) {
+        f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int h = 0; h < T; h++) {
+            const float scale[2] = {fp4_scale(t.ks[0][h]), fp4_scale(t.ks[1][h])};
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                bf16x8 q[QP];
+#pragma unroll
+                for (int part = 0; part < QP; part++) q[part] = query(part, h, i);
+#pragma unroll
+                for (int u = 0; u < 2; u++) {
+                    const bf16x8 k8 = widen_word(t.k[u][h][i], scale[u]);
+#pragma unroll
+                    for (int part = 0; part < QP; part++) s[u] = mfma_bf16(k8, q[part], s[u]);
+                }
+            }
+        }
+        if (NH == 2 && __builtin_amdgcn_ballot_w64(t.ks[0][0] == 255u || t.ks[1][0] == 255u)) {
+            // a block that reads as NaN must not reach the other head's columns (NaN times their zeros)
+#pragma unroll
+            for (int u = 0; u < 2; u++) {
+                f32x4 c[2];
+#pragma unroll
+                for (int sub = 0; sub < 2; sub++) {
+                    c[sub] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const bf16x8 k8 = widen_word(ksub == sub ? t.k[u][0][i] : 0u, ksub == sub ? fp4_scale(t.ks[u][0]) : 1.f);
+#pragma unroll
+                        for (int part = 0; part < QP; part++) c[sub] = mfma_bf16(k8, query(part, 0, i), c[sub]);
+                    }
+                }
+                s[u] = qsub ? c[1] : c[0];
+            }
+        }
+        float p[8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            const float one = s[e >> 2][e & 3];
+            p[e] = one;
+        }
+        if (rows < 32) {
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                if (16 * (e >> 2) + 4 * g + (e & 3) >= rows) p[e] = -INFINITY;
+        }
+        const float mx = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7]))) * a.scale_log2e;
+        if (__builtin_amdgcn_ballot_w64(mx > m + 8.f)) {  // (also where there is no reference yet)
+            const float mn = fmaxf(m, max_over_rows(mx));
+            const float alpha = fast_exp2(m - exp_reference(mn));
+            l *= alpha;
+#pragma unroll
+            for (int i = 0; i < 8 * T; i++) acc[i] *= alpha;
+            m = mn;
+        }
+        const float ref = exp_reference(m);
+#pragma unroll
+        for (int e = 0; e < 8; e++) p[e] = fast_exp2(fmaf(p[e], a.scale_log2e, -ref));
+        l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+        bf16x8 pw[NP];
+#pragma unroll
+        for (int part = 0; part < NP; part++) {
+            unsigned w[4];
+#pragma unroll
+            for (int e = 0; e < 4; e++) w[e] = take_bf16_part(p[2 * e], p[2 * e + 1]);
+            pw[part] = pack_words(w[0], w[1], w[2], w[3]);
+        }
+        float vs[8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) vs[e] = fp4_scale(t.vs[e]);
+#pragma unroll
+        for (int h = 0; h < T; h++) {
+            unsigned v[8];
+#pragma unroll
+            for (int e = 0; e < 8; e++) v[e] = t.v[e][h];
+            fold_pairs<0>(v, vs, pw, h);
+            fold_pairs<1>(v, vs, pw, h);
+            fold_pairs<2>(v, vs, pw, h);
+            fold_pairs<3>(v, vs, pw, h);
+        }
+    }
+    template <int B>
+    __device__ __forceinline__ void fold_pairs(const unsigned (&v)[8], const float (&vs)[8], const bf16x8 (&pw)[NP], int h) {
+        bf16x8 lo, hi;
+        widen_pairs<B>(v, vs, lo, hi);
+#pragma unroll
+        for (int part = 0; part < NP; part++) {
+            acc[8 * h + 2 * B] = mfma_bf16(lo, pw[part], acc[8 * h + 2 * B]);
+            acc[8 * h + 2 * B + 1] = mfma_bf16(hi, pw[part], acc[8 * h + 2 * B + 1]);
+        }
+    }
+
+    // A decode step's new row, still 16-bit, as the last of a tile's `rows` rows: its blocks are rounded by the lanes that use them and
+    // written to the arena (row `row`) by those that own the bytes.
+    __device__ __forceinline__ void take_new_row(Fp4Tile<W> &t, int b, int64_t row, int rows) const {
+        const int64_t at = row * row_bytes;
+        const bool k_own = r == 0 && (D != 64 || (NH == 2 ? ksub == 0 || second : g < 2));
+        const bool v_own = g == 0 && (D != 64 || (NH == 2 ? vsub == 0 || second : r < 8));
+        const char *ksrc = a.k_new + (((int64_t)b * a.H + khead) * D + kblk * 32) * 2;
+        const char *vsrc = a.v_new + (((int64_t)b * a.H + vhead) * D + vel) * 2;
+#pragma unroll
+        for (int h = 0; h < T; h++) {
+            float x[4][8];
+            unsigned most = 0;
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                widen8<ACT>(*(const u32x4 *)(ksrc + h * 256 + i * 16), x[i]);
+#pragma unroll
+                for (int e = 0; e < 8; e++) most = fp4_magnitude(x[i][e], most);
+            }
+            const unsigned byte = fp4_scale_byte<ACT>(__builtin_bit_cast(float, most));
+            u32x4 c;
+#pragma unroll
+            for (int i = 0; i < 4; i++) c[i] = fp4_codes8(x[i], byte);
+            if (k_own) {
+                *(u32x4 *)(a.kplane + at + ko + 64 * h) = c;
+                *(unsigned char *)(a.kplane + at + kso + 4 * h) = (unsigned char)byte;
+            }
+#pragma unroll
+            for (int u = 0; u < 2; u++)
+                if (16 * u + r >= rows - 1) {
+                    t.k[u][h] = c;
+                    t.ks[u][h] = byte;
+                }
+        }
+        float x[T][8];
+        unsigned most = 0;
+#pragma unroll
+        for (int h = 0; h < T; h++) {
+            widen8<ACT>(*(const u32x4 *)(vsrc + h * 16), x[h]);
+#pragma unroll
+            for (int e = 0; e < 8; e++) most = fp4_magnitude(x[h][e], most);
+        }
+        most = group_max<4 / T>(most);
+        const unsigned byte = fp4_scale_byte<ACT>(__builtin_bit_cast(float, most));
+#pragma unroll
+        for (int h = 0; h < T; h++) {
+            const unsigned c = fp4_codes8(x[h], byte);
+            if (v_own) *(unsigned *)(a.vplane + at + vo + 4 * h) = c;
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                if (16 * (e >> 2) + 4 * g + (e & 3) >= rows - 1) t.v[e][h] = c;
+        }
+        if (v_own && vel % 32 == 0) *(unsigned char *)(a.vplane + at + vso) = (unsigned char)byte;
+        const int used = code_bytes + a.H * (D / 32);
+        if (kh0 + NH >= a.H && lane < row_bytes - used) {  // zeros up to a multiple of 16 bytes
+            a.kplane[at + used + lane] = 0;
+            a.vplane[at + used + lane] = 0;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+            if (16 * (e >> 2) + 4 * g + (e & 3) >= rows - 1) t.vs[e] = byte;
+    }
+
+    // Four neighbouring elements of this lane's column, i < 2T, rr < 4: elements 8T * (4g + rr) + 4i .. + 3 of the unit.
+    __device__ __forceinline__ f32x4 sums4(int rr, int i) const {
+        f32x4 o;
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const float one = acc[4 * i + e][rr];
+            o[e] = one;
+        }
+        return o;
+    }
+};
+
+// The new lengths, and a zero output row for empty or refused contexts, by the workgroups in turn.
+template <int D>
+__device__ __forceinline__ void publish_lengths(const AttnArgs &a, const BatchView &bv) {
     for (int b = blockIdx.x; b < a.n; b += gridDim.x) {
         if (a.len_out && threadIdx.x == 0) a.len_out[b] = a.cur_len[b] + 1;
         if (bv.len[b] == 0) {
@@ -158,7 +413,26 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_kernel(const AttnArgs a) {
             for (int e = threadIdx.x; e < a.Hq * D / 8; e += 256) store_out8(a.out, a.out_dtype, ((int64_t)b * a.Hq * D / 8 + e) * 8, z);
         }
     }
-    const int code_bytes = fp4_code_bytes(a.H, D), row_bytes = fp4_row_bytes(a.H, D);
+}
+
+// Few (context, column) pairs: an item is a chunk of a context for a column, its rows shared out over the four waves of a workgroup,
+// which meet in LDS; chunks meet through memory.
+template <int ACT, int D, int NH, int NP>
+__global__ void __launch_bounds__(256, 2) attn_fp4_team_kernel(const AttnArgs a) {
+    typedef Fp4Wave<ACT, D, NH, NP> Wave;
+    constexpr int W = Wave::W, T = Wave::T, QB = Wave::QB, TS = 4;
+    constexpr int STRIDE = W + 4;  // floats of a column in LDS
+    extern __shared__ __align__(16) char dyn_lds[];  // the batch view, the queries, then the waves' sums of the columns in use
+    __shared__ int wave_sums[S3_MAX_CLASSES * S3_MAX_WAVES];
+    __shared__ float comb_m[TS][16], comb_l[TS][16];
+    __shared__ int last_of_context;
+    const int ts = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // (scalar: row ranges and buffers with it)
+    const BatchView bv = build_batch_view<false>(a, dyn_lds, wave_sums);
+    char *queries = dyn_lds + ((batch_view_bytes(a.n, a.ncls) + 15) & ~(size_t)15);
+    float *comb = (float *)(queries + Wave::Q_BYTES);
+    publish_lengths<D>(a, bv);
+    Wave w(a, queries);  // (the waves have the same queries: each writes all of them, so none waits for another)
+    const int row_bytes = w.row_bytes;
     // Work in the order of eighths: workgroup b (XCD b % 8) takes the chunks whose number leaves the same remainder, so that the
     // columns of a chunk, whose bytes share cache lines, are on one XCD's L2.
     const int64_t total = (int64_t)((bv.total + 7) / 8) * 8 * a.columns;
@@ -168,258 +442,58 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_kernel(const AttnArgs a) {
         if (chunk_no >= bv.total) continue;
         const int col = (int)(y % a.columns);
         const Item it = uniform_item(decode_item(a, bv, chunk_no, 1));
-        const int unit = col / a.nqb, qb = col - unit * a.nqb;
         const int start = it.c * it.clen, end = min(it.len, start + it.clen);
         const int per = (end - start + TS - 1) / TS;
         const int j0 = min(end, start + ts * per), j1 = min(end, j0 + per);
         const bool has_new = a.k_new != nullptr && j1 == it.len && j0 < j1;
-
-        // which heads: of the A operand's lanes (K: block group g; V: elements of lane m = r), of the B operand's columns
-        const int ksub = NH == 2 ? g >> 1 : 0, vsub = NH == 2 ? r >> 3 : 0, qsub = NH == 2 ? r >> 3 : 0;
-        const int kh0 = unit * NH;
-        const bool second = NH == 2 && kh0 + 1 < a.H;
-        const int khead = kh0 + (second ? ksub : 0), vhead = kh0 + (second ? vsub : 0);
-        const int kblk = D == 64 ? g & 1 : g;                // (+ 4 for the second half of 256)
-        const int vel = D == 256 ? 16 * r : D == 64 ? 8 * (r & 7) : 8 * r;  // first element of the V words
-        const int ko = khead * (D / 2) + kblk * 16, kso = code_bytes + khead * (D / 32) + kblk;
-        const int vo = vhead * (D / 2) + vel / 2, vso = code_bytes + vhead * (D / 32) + vel / 32;
-        const int qi = (r % QB) + qb * QB, qhead = (kh0 + qsub) * a.group + qi;
-        const bool column = qi < a.group && (NH == 1 || qsub == 0 || second);
-        const bool q_here = column && (D != 64 || (NH == 2 ? ksub == qsub : g < 2));
-
-        bf16x8 q[QP][T][4];
-#pragma unroll
-        for (int h = 0; h < T; h++)
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                u32x4 w = {0u, 0u, 0u, 0u};
-                if (q_here) w = *(const u32x4 *)(a.q + (((int64_t)it.b * a.Hq + qhead) * D + h * 128 + kblk * 32 + i * 8) * 2);
-                if (QP == 1) {
-                    q[0][h][i] = __builtin_bit_cast(bf16x8, w);
-                } else {
-                    float x[8];
-                    widen8<ACT>(w, x);
-                    unsigned p[QP][4];
-#pragma unroll
-                    for (int part = 0; part < QP; part++)
-#pragma unroll
-                        for (int e = 0; e < 4; e++) p[part][e] = take_bf16_part(x[2 * e], x[2 * e + 1]);
-#pragma unroll
-                    for (int part = 0; part < QP; part++) q[part][h][i] = pack_words(p[part][0], p[part][1], p[part][2], p[part][3]);
-                }
-            }
-
-        float m = -INFINITY, l = 0.f;
-        f32x4 acc[8 * T];
-#pragma unroll
-        for (int i = 0; i < 8 * T; i++) acc[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
-
+        w.set_column(col);
         const char *kp = a.kplane + (it.off + j0) * (int64_t)row_bytes, *vp = a.vplane + (it.off + j0) * (int64_t)row_bytes;
-        // what a tile holds is folded into (m, l, acc); rows: 32, or fewer in the last tile
-        auto fold = [&](const Fp4Tile<W> &t, int rows, bool full) {
-            f32x4 s[2];
-#pragma unroll
-            for (int u = 0; u < 2; u++) {
-                f32x4 c = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int h = 0; h < T; h++) {
-                    const float scale = fp4_scale(t.ks[u][h]);
-#pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        const bf16x8 k8 = widen_word(t.k[u][h][i], scale);
-#pragma unroll
-                        for (int part = 0; part < QP; part++) c = mfma_bf16(k8, q[part][h][i], c);
-                    }
-                }
-                s[u] = c;
-            }
-            if (NH == 2 && __builtin_amdgcn_ballot_w64(t.ks[0][0] == 255u || t.ks[1][0] == 255u)) {
-                // a block that reads as NaN must not reach the other head's columns (NaN times their zeros)
-#pragma unroll
-                for (int u = 0; u < 2; u++) {
-                    f32x4 c[2];
-#pragma unroll
-                    for (int sub = 0; sub < 2; sub++) {
-                        c[sub] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                        for (int i = 0; i < 4; i++) {
-                            const bf16x8 k8 = widen_word(ksub == sub ? t.k[u][0][i] : 0u, ksub == sub ? fp4_scale(t.ks[u][0]) : 1.f);
-#pragma unroll
-                            for (int part = 0; part < QP; part++) c[sub] = mfma_bf16(k8, q[part][0][i], c[sub]);
-                        }
-                    }
-                    s[u] = qsub ? c[1] : c[0];
-                }
-            }
-            float p[8], mx = -INFINITY;
-#pragma unroll
-            for (int e = 0; e < 8; e++) {
-                p[e] = s[e >> 2][e & 3] * a.scale_log2e;
-                if (!full && 16 * (e >> 2) + 4 * g + (e & 3) >= rows) p[e] = -INFINITY;
-                mx = fmaxf(mx, p[e]);
-            }
-            if (__builtin_amdgcn_ballot_w64(mx > m + 8.f)) {  // (also where there is no reference yet)
-                const float mn = fmaxf(m, max_over_rows(mx));
-                const float alpha = fast_exp2(m - exp_reference(mn));
-                l *= alpha;
-#pragma unroll
-                for (int i = 0; i < 8 * T; i++) acc[i] *= alpha;
-                m = mn;
-            }
-            const float ref = exp_reference(m);
-#pragma unroll
-            for (int e = 0; e < 8; e++) {
-                p[e] = fast_exp2(p[e] - ref);
-                l += p[e];
-            }
-            bf16x8 pw[NP];
-#pragma unroll
-            for (int part = 0; part < NP; part++) {
-                unsigned w[4];
-#pragma unroll
-                for (int e = 0; e < 4; e++) w[e] = take_bf16_part(p[2 * e], p[2 * e + 1]);
-                pw[part] = pack_words(w[0], w[1], w[2], w[3]);
-            }
-            float vs[8];
-#pragma unroll
-            for (int e = 0; e < 8; e++) vs[e] = fp4_scale(t.vs[e]);
-#pragma unroll
-            for (int h = 0; h < T; h++) {
-                unsigned v[8];
-#pragma unroll
-                for (int e = 0; e < 8; e++) v[e] = t.v[e][h];
-                bf16x8 lo, hi;
-#define S3_FP4_PAIR(B)                                                                            \
-    widen_pairs<B>(v, vs, lo, hi);                                                                \
-    _Pragma("unroll") for (int part = 0; part < NP; part++) {                                     \
-        acc[8 * h + 2 * B] = mfma_bf16(lo, pw[part], acc[8 * h + 2 * B]);                         \
-        acc[8 * h + 2 * B + 1] = mfma_bf16(hi, pw[part], acc[8 * h + 2 * B + 1]);                 \
-    }
-                S3_FP4_PAIR(0)
-                S3_FP4_PAIR(1)
-                S3_FP4_PAIR(2)
-                S3_FP4_PAIR(3)
-#undef S3_FP4_PAIR
-            }
-        };
+        const int64_t step = 32 * (int64_t)row_bytes, new_row = it.off + it.len - 1;
+        // Two tiles' registers in turn, so that the next tile's loads are out while one is folded in.
         Fp4Tile<W> t0, t1;
-        const int rows_all = j1 - j0, full_tiles = max(0, rows_all - (has_new ? 1 : 0)) / 32;
-        const int tail = rows_all - 32 * full_tiles;  // 0 .. 32 rows, the new one among them
-        if (full_tiles > 0) {
-            load_tile<W, true>(t0, kp, vp, row_bytes, 32, ko, kso, vo, vso);
-            for (int i = 0; i < full_tiles; i += 2) {
-                if (i + 1 < full_tiles) load_tile<W, true>(t1, kp + (int64_t)(i + 1) * 32 * row_bytes, vp + (int64_t)(i + 1) * 32 * row_bytes, row_bytes, 32, ko, kso, vo, vso);
-                fold(t0, 32, true);
-                if (i + 1 >= full_tiles) break;
-                if (i + 2 < full_tiles) load_tile<W, true>(t0, kp + (int64_t)(i + 2) * 32 * row_bytes, vp + (int64_t)(i + 2) * 32 * row_bytes, row_bytes, 32, ko, kso, vo, vso);
-                fold(t1, 32, true);
-            }
-        }
-        if (tail > 0) {
-            const int64_t skip = (int64_t)full_tiles * 32 * row_bytes;
-            load_tile<W, false>(t0, kp + skip, vp + skip, row_bytes, tail, ko, kso, vo, vso);
-            if (has_new) {
-                // The new row, still 16-bit: its blocks are rounded by the lanes that use them and written to the arena by those
-                // that own the bytes; rows tail-1 and beyond of the tile read it.
-                const int64_t row = (it.off + it.len - 1) * (int64_t)row_bytes;
-                const bool k_own = r == 0 && (D != 64 || (NH == 2 ? ksub == 0 || second : g < 2));
-                const bool v_own = g == 0 && (D != 64 || (NH == 2 ? vsub == 0 || second : r < 8));
-                const char *ks = a.k_new + (((int64_t)it.b * a.H + khead) * D + kblk * 32) * 2;
-                const char *vsrc = a.v_new + (((int64_t)it.b * a.H + vhead) * D + vel) * 2;
-#pragma unroll
-                for (int h = 0; h < T; h++) {
-                    float x[4][8];
-                    unsigned most = 0;
-#pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        widen8<ACT>(*(const u32x4 *)(ks + h * 256 + i * 16), x[i]);
-#pragma unroll
-                        for (int e = 0; e < 8; e++) most = fp4_magnitude(x[i][e], most);
-                    }
-                    const unsigned byte = fp4_scale_byte<ACT>(__builtin_bit_cast(float, most));
-                    u32x4 c;
-#pragma unroll
-                    for (int i = 0; i < 4; i++) c[i] = fp4_codes8(x[i], byte);
-                    if (k_own) {
-                        *(u32x4 *)(a.kplane + row + ko + 64 * h) = c;
-                        *(unsigned char *)(a.kplane + row + kso + 4 * h) = (unsigned char)byte;
-                    }
-#pragma unroll
-                    for (int u = 0; u < 2; u++)
-                        if (16 * u + r >= tail - 1) {
-                            t0.k[u][h] = c;
-                            t0.ks[u][h] = byte;
-                        }
-                }
-                float x[T][8];
-                unsigned most = 0;
-#pragma unroll
-                for (int h = 0; h < T; h++) {
-                    widen8<ACT>(*(const u32x4 *)(vsrc + h * 16), x[h]);
-#pragma unroll
-                    for (int e = 0; e < 8; e++) most = fp4_magnitude(x[h][e], most);
-                }
-                most = group_max<4 / T>(most);
-                const unsigned byte = fp4_scale_byte<ACT>(__builtin_bit_cast(float, most));
-#pragma unroll
-                for (int h = 0; h < T; h++) {
-                    const unsigned c = fp4_codes8(x[h], byte);
-                    if (v_own) *(unsigned *)(a.vplane + row + vo + 4 * h) = c;
-#pragma unroll
-                    for (int e = 0; e < 8; e++)
-                        if (16 * (e >> 2) + 4 * g + (e & 3) >= tail - 1) t0.v[e][h] = c;
-                }
-                if (v_own && vel % 32 == 0) *(unsigned char *)(a.vplane + row + vso) = (unsigned char)byte;
-                const int used = code_bytes + a.H * (D / 32);
-                if (kh0 + NH >= a.H && lane < row_bytes - used) {  // zeros up to a multiple of 16 bytes
-                    a.kplane[row + used + lane] = 0;
-                    a.vplane[row + used + lane] = 0;
-                }
-#pragma unroll
-                for (int e = 0; e < 8; e++)
-                    if (16 * (e >> 2) + 4 * g + (e & 3) >= tail - 1) t0.vs[e] = byte;
-            }
-            fold(t0, tail, false);
+        w.load(t0, kp, vp, j1 - j0);
+        w.begin(it.b);
+        for (int left = j1 - j0; left > 0; left -= 64) {
+            w.load(t1, kp + step, vp + step, left - 32);
+            if (has_new && left <= 32) w.take_new_row(t0, it.b, new_row, left);
+            w.fold(t0, left);
+            if (left <= 32) break;
+            kp += 2 * step;
+            vp += 2 * step;
+            w.load(t0, kp, vp, left - 64);
+            if (has_new && left <= 64) w.take_new_row(t1, it.b, new_row, left - 32);
+            w.fold(t1, left - 32);
         }
 
         // the four waves meet: columns in use, compact (head, query)
-        const int per_head = min(a.group - qb * QB, QB);
-        const int slot = qsub * per_head + (r % QB), n_cols = (second ? 2 : 1) * per_head;
-        l = sum_over_rows(l);
-        if (column && g == 0) {
-            comb_m[ts][slot] = m;
+        const int slot = w.qsub * w.per_head + (w.r % QB), n_cols = (w.second ? 2 : 1) * w.per_head;
+        const float l = sum_over_rows(w.l);
+        if (w.column && w.g == 0) {
+            comb_m[ts][slot] = w.m;
             comb_l[ts][slot] = l;
         }
-        if (column) {
+        if (w.column) {
 #pragma unroll
             for (int rr = 0; rr < 4; rr++)
 #pragma unroll
-                for (int h = 0; h < 2 * T; h++) {
-                    // elements 8T * (4g + rr) + 4h .. + 3 of the unit
-                    f32x4 o;
-#pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        const float one = acc[4 * h + e][rr];
-                        o[e] = one;
-                    }
-                    *(f32x4 *)(comb + ((size_t)ts * n_cols + slot) * STRIDE + 8 * T * (4 * g + rr) + 4 * h) = o;
-                }
+                for (int i = 0; i < 2 * T; i++)
+                    *(f32x4 *)(comb + ((size_t)ts * n_cols + slot) * STRIDE + 8 * T * (4 * w.g + rr) + 4 * i) = w.sums4(rr, i);
         }
         __syncthreads();
         // a thread: eight elements of one column
         const int slices = n_cols * (D / 8);
         for (int i = threadIdx.x; i < slices; i += 256) {
-            const int c = i / (D / 8), dl = i % (D / 8), sub = NH == 2 && c >= per_head ? 1 : 0;
-            const int h = (kh0 + sub) * a.group + qb * QB + (c - sub * per_head);
+            const int c = i / (D / 8), dl = i % (D / 8), sub = NH == 2 && c >= w.per_head ? 1 : 0;
+            const int h = (w.kh0 + sub) * a.group + w.qb * QB + (c - sub * w.per_head);
             float mm = -INFINITY, ll = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < TS; w++) mm = fmaxf(mm, comb_m[w][c]);
+            for (int x = 0; x < TS; x++) mm = fmaxf(mm, comb_m[x][c]);
             const float ref = exp_reference(mm);
 #pragma unroll
-            for (int w = 0; w < TS; w++) {
-                const float wt = fast_exp2(comb_m[w][c] - ref);
-                ll += wt * comb_l[w][c];
-                const float *src = comb + ((size_t)w * n_cols + c) * STRIDE + sub * 64 + dl * 8;
+            for (int x = 0; x < TS; x++) {
+                const float wt = fast_exp2(comb_m[x][c] - ref);
+                ll += wt * comb_l[x][c];
+                const float *src = comb + ((size_t)x * n_cols + c) * STRIDE + sub * 64 + dl * 8;
                 const f32x4 x0 = *(const f32x4 *)src, x1 = *(const f32x4 *)(src + 4);
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
@@ -446,14 +520,14 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_kernel(const AttnArgs a) {
             __syncthreads();
             if (ts == 0) {
                 const bool last = chunk_arrived(a, arrival_counter(a, it.b, a.columns, col), it.nchunks);
-                if (lane == 0) last_of_context = last;
+                if (w.lane == 0) last_of_context = last;
             }
             __syncthreads();
             if (last_of_context) {
                 if (a.merge_sync) __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
                 for (int i = threadIdx.x; i < slices; i += 256) {
-                    const int c = i / (D / 8), dl = i % (D / 8), sub = NH == 2 && c >= per_head ? 1 : 0;
-                    merge_chunks<D, true>(a, it.slot0, a.Hq, it.b, (kh0 + sub) * a.group + qb * QB + (c - sub * per_head), dl, it.nchunks);
+                    const int c = i / (D / 8), dl = i % (D / 8), sub = NH == 2 && c >= w.per_head ? 1 : 0;
+                    merge_chunks<D, true>(a, it.slot0, a.Hq, it.b, (w.kh0 + sub) * a.group + w.qb * QB + (c - sub * w.per_head), dl, it.nchunks);
                 }
             }
         }
@@ -461,18 +535,165 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_kernel(const AttnArgs a) {
     }
 }
 
-template <int ACT, int NP>
-static attn_fn pick_fp4(int d, int nh) {
-    if (d == 64) return nh == 2 ? attn_fp4_kernel<ACT, 64, 2, NP> : attn_fp4_kernel<ACT, 64, 1, NP>;
-    if (d == 128) return attn_fp4_kernel<ACT, 128, 1, NP>;
-    if (d == 256) return attn_fp4_kernel<ACT, 256, 1, NP>;
-    return nullptr;
+// Many (context, column) pairs: the tiles of all contexts laid end to end are cut into equal shares, one a wave and column, so that
+// waves end together whatever the lengths, and no wave waits for another.  A share runs through whole contexts, which it finishes by
+// itself, and at either end through a part of one that others share: such a piece goes to memory (share u's piece of context b to slot
+// u + b: along the shares either u or b grows, so no two meet), is counted, and whoever counts the last piece of a context merges them.
+// Contexts of few tiles are not cut: a share takes those that begin in it.
+#define S3_FP4_UNCUT 8
+template <int ACT, int D, int NH, int NP>
+__global__ void __launch_bounds__(256, 2) attn_fp4_share_kernel(const AttnArgs a) {
+    typedef Fp4Wave<ACT, D, NH, NP> Wave;
+    constexpr int W = Wave::W, T = Wave::T, QB = Wave::QB;
+    extern __shared__ __align__(16) char dyn_lds[];  // the batch view in tiles, then the waves' queries
+    __shared__ int wave_sums[3 * S3_MAX_WAVES];
+    int longest = 0;
+    const BatchView bv = build_tile_view<32>(a, dyn_lds, wave_sums, longest);
+    char *queries = dyn_lds + ((batch_view_bytes(a.n, 1) + 15) & ~(size_t)15);
+    publish_lengths<D>(a, bv);
+    const int ts = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // Neighbouring columns, whose bytes share cache lines, are on neighbouring waves, and those on one XCD (workgroup b is on XCD b % 8).
+    const int rank = (gridDim.x & 7) == 0 ? (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3) : blockIdx.x;
+    const int place = rank * 4 + ts;
+    const int share = place / a.columns, col = place - share * a.columns;
+    const int total = __builtin_amdgcn_readfirstlane(bv.total);
+    const bool cut = __builtin_amdgcn_readfirstlane(longest) > 32 * S3_FP4_UNCUT;
+    const int size = max((total + a.wave_shares - 1) / a.wave_shares, 1);
+    if (share >= a.wave_shares || share * (int64_t)size >= total) return;
+    int t0 = share * size, t1 = min(total, t0 + size);
+    int b = __builtin_amdgcn_readfirstlane(find_sequence(bv.pre, a.n, t0));  // the context that holds tile t0
+    if (!cut) {  // from the first context that begins at t0 or behind it to the last that begins in front of t1
+        if (__builtin_amdgcn_readfirstlane(bv.pre[b]) < t0) b++;
+        t0 = __builtin_amdgcn_readfirstlane(bv.pre[b]);
+        if (t0 >= t1) return;
+        t1 = __builtin_amdgcn_readfirstlane(bv.pre[find_sequence(bv.pre, a.n, t1 - 1) + 1]);
+    }
+    Wave w(a, queries + ts * Wave::Q_BYTES);
+    w.set_column(col);
+    const int row_bytes = w.row_bytes;
+    Pending head = {0, 0, 0}, tail = {0, 0, 0};  // pieces of the contexts that the share's borders cut
+
+    // the loader: context, its first tile, rows from the tile to load on (0: the share is loaded)
+    struct Cursor {
+        int b, begin, end;  // tiles of context b
+        int tile, len;
+        int64_t off;
+    };
+    const auto open = [&](Cursor &c, int tile) {  // the context that holds `tile`, from context c.b on
+        while (true) {
+            c.end = __builtin_amdgcn_readfirstlane(bv.pre[c.b + 1]);
+            if (tile < c.end) break;
+            c.b++;
+        }
+        c.begin = __builtin_amdgcn_readfirstlane(bv.pre[c.b]);
+        c.len = __builtin_amdgcn_readfirstlane(bv.len[c.b]);
+        c.off = uniform64(bv.off[c.b]);
+        c.tile = tile;
+    };
+    const auto load = [&](Fp4Tile<W> &t, const Cursor &c, bool there) {
+        const int64_t row = c.off + (int64_t)(c.tile - c.begin) * 32;
+        w.load(t, a.kplane + row * row_bytes, a.vplane + row * row_bytes, there ? c.len - (c.tile - c.begin) * 32 : 0);
+    };
+    const auto finish = [&](const Cursor &c) {  // the share's part of context c.b is folded in
+        const int first = max(c.begin, t0), last = min(c.end, t1);
+        const float l = sum_over_rows(w.l);
+        const bool mine = w.column && (D != 64 || (NH == 2 ? (w.g >> 1) == w.qsub : w.g < 2));
+        const int e0 = 8 * T * 4 * w.g - (NH == 2 ? 64 * w.qsub : 0);  // this lane's first element of its head
+        if (first == c.begin && last == c.end) {
+            const float inv = 1.f / l;
+            if (mine) {
+#pragma unroll
+                for (int rr = 0; rr < 4; rr++)
+#pragma unroll
+                    for (int i = 0; i < T; i++) {
+                        const f32x4 lo = w.sums4(rr, 2 * i), hi = w.sums4(rr, 2 * i + 1);
+                        const float o[8] = {lo[0] * inv, lo[1] * inv, lo[2] * inv, lo[3] * inv, hi[0] * inv, hi[1] * inv, hi[2] * inv, hi[3] * inv};
+                        store_out8(a.out, a.out_dtype, ((int64_t)c.b * a.Hq + w.qhead) * D + e0 + 8 * T * rr + 8 * i, o);
+                    }
+            }
+            return;
+        }
+        const int u0 = c.begin / size, u1 = (c.end - 1) / size;
+        const Pending p = {c.b, u0, u1 - u0 + 1};
+        if (first == t0) head = p;
+        else tail = p;
+        if (mine) {
+            const int64_t pi = (int64_t)(share + c.b) * a.Hq + w.qhead;
+            if (e0 == 0) put_partial2<true>((float *)a.part_ml + 2 * pi, (f32x2){w.m, l});
+            float *pa = a.part_acc + pi * D + e0;
+#pragma unroll
+            for (int rr = 0; rr < 4; rr++)
+#pragma unroll
+                for (int i = 0; i < 2 * T; i++) put_partial4<true>(pa + 8 * T * rr + 4 * i, w.sums4(rr, i));
+        }
+    };
+    // one tile: the next one's loads leave, then this one is folded in
+    Cursor now;
+    now.b = b;
+    open(now, t0);
+    const auto advance = [&](const Cursor &c, Fp4Tile<W> &t) {
+        Cursor n = c;
+        const bool there = c.tile + 1 < t1;
+        if (there) {
+            if (c.tile + 1 < c.end) n.tile++;
+            else open(n, c.tile + 1);
+        }
+        load(t, n, there);
+        return n;
+    };
+    const auto one = [&](Fp4Tile<W> &t, const Cursor &c, int next_b) {
+        const int rows = c.len - (c.tile - c.begin) * 32;
+        if (a.k_new != nullptr && rows <= 32) w.take_new_row(t, c.b, c.off + c.len - 1, rows);
+        w.fold(t, rows);
+        const bool last = c.tile + 1 == t1;
+        if (last || c.tile + 1 == c.end) {
+            finish(c);
+            if (!last) w.begin(next_b);
+        }
+    };
+    Fp4Tile<W> ta, tb;
+    load(ta, now, true);
+    w.begin(now.b);
+    while (true) {
+        Cursor next = advance(now, tb);
+        one(ta, now, next.b);
+        if (now.tile + 1 >= t1) break;
+        now = advance(next, ta);
+        one(tb, next, now.b);
+        if (next.tile + 1 >= t1) break;
+    }
+    if (head.count + tail.count == 0) return;
+    const unsigned who = pieces_arrived(a, head, tail, a.columns, col);
+#pragma unroll 1
+    for (int k = 0; k < 2; k++) {
+        if (!(who >> k & 1)) continue;
+        const Pending p = {k ? tail.b : head.b, k ? tail.first : head.first, k ? tail.count : head.count};
+        const int slices = (w.second ? 2 : 1) * w.per_head * (D / 8);
+        for (int i = w.lane; i < slices; i += 64) {
+            const int c = i / (D / 8), dl = i % (D / 8), sub = NH == 2 && c >= w.per_head ? 1 : 0;
+            merge_chunks<D, true>(a, p.first + p.b, a.Hq, p.b, (w.kh0 + sub) * a.group + w.qb * QB + (c - sub * w.per_head), dl, p.count);
+        }
+    }
 }
 
-attn_fn s3i_pick_fp4(int act, int d, int heads_per_unit, bool wide_out) {
-    if (act == S3_F16) return wide_out ? pick_fp4<S3_F16, 3>(d, heads_per_unit) : pick_fp4<S3_F16, 2>(d, heads_per_unit);
-    if (act == S3_BF16) return wide_out ? pick_fp4<S3_BF16, 3>(d, heads_per_unit) : pick_fp4<S3_BF16, 2>(d, heads_per_unit);
-    return nullptr;
+template <int ACT, int NP, bool SHARES>
+static attn_fn pick_fp4(int d, int nh) {
+    if (SHARES) {
+        if (d == 64) return nh == 2 ? attn_fp4_share_kernel<ACT, 64, 2, NP> : attn_fp4_share_kernel<ACT, 64, 1, NP>;
+        return d == 128 ? attn_fp4_share_kernel<ACT, 128, 1, NP> : d == 256 ? attn_fp4_share_kernel<ACT, 256, 1, NP> : nullptr;
+    }
+    if (d == 64) return nh == 2 ? attn_fp4_team_kernel<ACT, 64, 2, NP> : attn_fp4_team_kernel<ACT, 64, 1, NP>;
+    return d == 128 ? attn_fp4_team_kernel<ACT, 128, 1, NP> : d == 256 ? attn_fp4_team_kernel<ACT, 256, 1, NP> : nullptr;
+}
+
+attn_fn s3i_pick_fp4(int act, int d, int heads_per_unit, bool wide_out, bool shares, int *query_bytes) {
+    *query_bytes = (shares ? 4 : 1) * (act == S3_F16 ? 2 : 1) * (d == 256 ? 2 : 1) * 4096;
+    if (act == S3_F16) {
+        if (wide_out) return shares ? pick_fp4<S3_F16, 3, true>(d, heads_per_unit) : pick_fp4<S3_F16, 3, false>(d, heads_per_unit);
+        return shares ? pick_fp4<S3_F16, 2, true>(d, heads_per_unit) : pick_fp4<S3_F16, 2, false>(d, heads_per_unit);
+    }
+    if (wide_out) return shares ? pick_fp4<S3_BF16, 3, true>(d, heads_per_unit) : pick_fp4<S3_BF16, 3, false>(d, heads_per_unit);
+    return shares ? pick_fp4<S3_BF16, 2, true>(d, heads_per_unit) : pick_fp4<S3_BF16, 2, false>(d, heads_per_unit);
 }
 
 append_fp8_fn s3i_pick_append_fp4(int act) {

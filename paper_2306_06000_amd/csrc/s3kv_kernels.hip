@@ -749,9 +749,10 @@ static size_t chunk_slots(const s3_arena *a, int n, int n_hg, size_t slot_bytes,
 // list) is a unit and up to sixteen (eight a head) of its query heads.
 struct Fp4Plan {
     int heads_per_unit, blocks_per_head, columns, used;  // used: matrix columns that carry query heads
-    int32_t few;                                         // chunks that few contexts are cut into, 0: chunks of `chunk` rows
+    bool shares;    // equal shares of all rows, one a wave (attn_fp4_share_kernel), or chunks of contexts, one a workgroup
+    int32_t few;    // chunks that few contexts are cut into, 0: chunks of `chunk` rows
     int chunk;
-    size_t slots;
+    size_t slots;   // of pieces
 };
 static Fp4Plan fp4_plan(const s3_arena *a, int n) {
     Fp4Plan p;
@@ -763,11 +764,18 @@ static Fp4Plan fp4_plan(const s3_arena *a, int n) {
     p.columns = (Hkv + p.heads_per_unit - 1) / p.heads_per_unit * p.blocks_per_head;
     p.used = p.heads_per_unit * (group < width ? group : width);
     p.chunk = a->chunk > 0 ? a->chunk : 1024;
+    const size_t slot_bytes = (size_t)a->cfg.n_heads * ((size_t)D * sizeof(float) + sizeof(float2));
+    const int64_t fixed = (int64_t)((S3_STATIC_SCRATCH_BYTES - counters_bytes(p.columns)) / slot_bytes);
+    const int64_t most = 8 * cus / p.columns;  // shares of a column: a wave each, eight waves a compute unit
+    p.shares = a->chunk <= 0 && a->grid_blocks <= 0 && p.columns <= 4 * cus && n * (int64_t)p.columns >= 4 * cus;
+    p.few = 0;
+    if (p.shares) {
+        p.slots = (size_t)(most + n);
+        return p;
+    }
     const int64_t whole = (int64_t)n * ((a->cfg.max_len + p.chunk - 1) / p.chunk);
     const int64_t fit = 2 * cus / p.columns;  // workgroups of a column that run at once
     int64_t want = a->chunk <= 0 && n < fit ? fit : 0;
-    const size_t slot_bytes = (size_t)a->cfg.n_heads * ((size_t)D * sizeof(float) + sizeof(float2));
-    const int64_t fixed = (int64_t)((S3_STATIC_SCRATCH_BYTES - counters_bytes(p.columns)) / slot_bytes);
     if (whole <= fixed && want > fixed - n) want = fixed - n;
     p.few = want > 0 ? (int32_t)want : 0;
     p.slots = (size_t)(want > 0 && want + n > whole ? want + n : whole);
@@ -1015,19 +1023,31 @@ static int launch_fp8(s3_arena *a, const AttnCall &c) {
 static int launch_fp4(s3_arena *a, const AttnCall &c) {
     const int D = a->cfg.head_dim;
     const Fp4Plan p = fp4_plan(a, c.n);
-    attn_fn fn = s3i_pick_fp4(a->cfg.act_dtype, D, p.heads_per_unit, c.out_dtype == S3_F32);
+    int query_bytes = 0;
+    attn_fn fn = s3i_pick_fp4(a->cfg.act_dtype, D, p.heads_per_unit, c.out_dtype == S3_F32, p.shares, &query_bytes);
     if (!fn) return S3_ERR_INVALID;
-    AttnArgs args = common_args(a, c, a->cfg.n_kv_heads, a->cfg.n_heads, p.chunk);
+    AttnArgs args = common_args(a, c, a->cfg.n_kv_heads, a->cfg.n_heads, p.shares ? 32 : p.chunk);
     args.few_chunks = p.few;
     args.group = a->cfg.n_heads / a->cfg.n_kv_heads;
     args.nqb = p.blocks_per_head;
     args.columns = p.columns;
     int rc = place_scratch(a, args, counters_bytes(p.columns), p.slots, c);
     if (rc != S3_OK) return rc;
-    // LDS: the batch view, and the sums of four waves
-    const size_t pieces = 4 * (size_t)p.used * ((D == 256 ? 256 : 128) + 4) * sizeof(float);
-    while (args.ncls > 1 && batch_view_lds(c.n, args.ncls) + pieces > (size_t)144 * 1024) args.ncls--;
-    const size_t dyn_lds = ((batch_view_lds(c.n, args.ncls) + 15) & ~(size_t)15) + pieces;
+    const int cus = a->num_cus > 0 ? a->num_cus : 256;
+    if (p.shares) {
+        args.ncls = 1;
+        const size_t dyn_lds = ((batch_view_lds(c.n, 1) + 15) & ~(size_t)15) + query_bytes;
+        int per_cu = 0;
+        rc = resident_per_cu((const void *)fn, 256, dyn_lds, &per_cu);
+        if (rc != S3_OK) return rc;
+        if (per_cu > 2) per_cu = 2;
+        args.wave_shares = 4 * cus * per_cu / p.columns;
+        return launch_attn_kernels(a, fn, cus * per_cu, 256, dyn_lds, c.stream, args, 0, !c.static_scratch);
+    }
+    // LDS: the batch view, the queries, and the sums of four waves
+    const size_t more = query_bytes + 4 * (size_t)p.used * ((D == 256 ? 256 : 128) + 4) * sizeof(float);
+    while (args.ncls > 1 && batch_view_lds(c.n, args.ncls) + more > (size_t)144 * 1024) args.ncls--;
+    const size_t dyn_lds = ((batch_view_lds(c.n, args.ncls) + 15) & ~(size_t)15) + more;
     int blocks = 0;
     rc = stride_grid(a, (const void *)fn, 256, dyn_lds, 1, &blocks);
     if (rc != S3_OK) return rc;

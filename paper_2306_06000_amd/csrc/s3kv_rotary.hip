@@ -36,6 +36,8 @@ struct RotaryArgs {
     uint64_t axes[4];    // two bits a pair
 };
 
+static bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
 // sin and cos of 2 pi x, |x| <= 1/2: the nearest quarter of a turn, and Taylor's sums for the rest (at most pi/4; the terms left out
 // are below 2^-29).
 __device__ __forceinline__ void sin_cos_turn(const float x, float &s, float &c) {
@@ -90,24 +92,55 @@ __device__ __forceinline__ void store_row8(char *row, int heads, int h, int e, c
     }
 }
 
-template <int ACT, int D, int CACHE>
+// Eight consecutive floats (PIECE: 16-byte aligned ones from w[at[0]] on) of a norm's weight.
+template <bool PIECE>
+__device__ __forceinline__ void load_weight8(const float *w, const int (&at)[8], float (&x)[8]) {
+    if (PIECE) {
+        const f32x4 lo = *(const f32x4 *)(w + at[0]), hi = *(const f32x4 *)(w + at[0] + 4);
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            x[i] = lo[i];
+            x[4 + i] = hi[i];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++) x[i] = w[at[i]];
+    }
+}
+
+// PAIRS: where the other elements of a lane's pairs are: 0 in the lane (interleaved), 1 in one 16-byte piece (half of the elements that
+// turn a multiple of 8), 2 anywhere.
+template <int ACT, int D, int CACHE, int PAIRS>
 __global__ void __launch_bounds__(256) rotary_kernel(const RotaryArgs a) {
     constexpr int LPH = D == 96 ? 16 : D / 8;  // lanes a head (of 96: twelve of sixteen)
     constexpr int GH = 64 / LPH;               // heads a wave takes at once
     const int lane = threadIdx.x & 63, sub = lane / LPH, e0 = (lane % LPH) * 8;
     const bool lane_ok = D != 96 || e0 < D;
     const int e = lane_ok ? e0 : 0;
-    const int heads = a.Hq + a.Hkv + (CACHE == S3_ROT_NONE ? 0 : a.Hkv);  // queries, keys, values
-    const int groups = (heads + GH - 1) / GH;
     const int64_t row_bytes = CACHE == S3_ROT_MXFP4 ? fp4_row_bytes(a.Hkv, D) : (int64_t)a.Hkv * D * (CACHE == S3_ROT_E4M3 ? 1 : 2);
-    // Where the pairs of this lane's elements are: first element of the pair's other halves, and whether they lie in one 16-byte piece
     const int half = a.rotary / 2;
-    const bool turns = e < a.rotary;
-    const bool in_lane = a.interleaved != 0;
-    const bool aligned = (half & 7) == 0;
+    // this lane's elements: turns per position, axis and other element of the pair, whatever the token
+    double rate[8];
+    int mine[8], other[8];
+    unsigned axis = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const int el = e + i;
+        const bool second = PAIRS == 0 ? el & 1 : el >= half;
+        const int pair = PAIRS == 0 ? el >> 1 : second ? el - half : el;
+        rate[i] = 0.0;
+        mine[i] = other[i] = el;
+        if (el < a.rotary) {
+            rate[i] = (double)a.inv_freq[pair] * 0.15915494309189533577;
+            axis |= (unsigned)((a.axes[pair >> 5] >> (2 * (pair & 31))) & 3) << (2 * i);
+            other[i] = PAIRS == 0 ? el ^ 1 : second ? el - half : el + half;
+        }
+    }
+    const int gq = (a.Hq + GH - 1) / GH, gk = (a.Hkv + GH - 1) / GH;
+    const unsigned lane_at = (unsigned)(sub * D + e) * 2, other_at = (unsigned)(sub * D + other[0]) * 2;
     for (int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); item < (int64_t)a.n * a.parts; item += (int64_t)gridDim.x * 4) {
-        const int64_t t = item / a.parts;
-        const int part = (int)(item - t * a.parts);
+        const int64_t t = uniform64(a.parts == 1 ? item : item / a.parts);
+        const int part = __builtin_amdgcn_readfirstlane((int)(item - t * a.parts));
         int64_t row = 0;
         int32_t p = 0;
         if (CACHE != S3_ROT_NONE) {
@@ -117,93 +150,138 @@ __global__ void __launch_bounds__(256) rotary_kernel(const RotaryArgs a) {
             row = (off + p) * row_bytes;
         }
         float cs[8], sn[8];
-        int other[8];
+        {
+            int32_t at[4];
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const int el = e + i;
-            const int pair = a.interleaved ? el >> 1 : el < half ? el : el - half;
-            const bool second = a.interleaved ? el & 1 : el >= half;
-            cs[i] = 1.f;
-            sn[i] = 0.f;
-            other[i] = el;
-            if (el < a.rotary) {
-                const int axis = (int)(a.axes[pair >> 5] >> (2 * (pair & 31))) & 3;
-                const int32_t at = a.rot_pos ? a.rot_pos[(int64_t)axis * a.n + t] : p;
-                double turn = (double)at * ((double)a.inv_freq[pair] * 0.15915494309189533577);
+            for (int x = 0; x < 4; x++) at[x] = a.rot_pos && a.rotary ? a.rot_pos[(int64_t)min(x, a.n_axes - 1) * a.n + t] : p;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const unsigned ax = (axis >> (2 * i)) & 3;
+                double turn = (double)(ax & 2 ? ax & 1 ? at[3] : at[2] : ax & 1 ? at[1] : at[0]) * rate[i];
                 turn -= rint(turn);
-                float s;
-                sin_cos_turn((float)turn, s, cs[i]);
-                sn[i] = second ? s : -s;
-                other[i] = a.interleaved ? el ^ 1 : second ? el - half : el + half;
+                sin_cos_turn((float)turn, sn[i], cs[i]);
+                const bool second = PAIRS == 0 ? i & 1 : e + i >= half;
+                if (!second) sn[i] = -sn[i];  // (elements that do not turn: no angle, cosine 1, sine 0)
             }
         }
-        for (int hg = part; hg < groups; hg += a.parts) {
-            const int hh = hg * GH + sub;
-            const bool ok = lane_ok && hh < heads;
-            const int kind = hh < a.Hq ? 0 : hh < a.Hq + a.Hkv ? 1 : 2;  // queries, keys, values
-            const int h = kind == 0 ? hh : kind == 1 ? hh - a.Hq : hh - a.Hq - a.Hkv;
-            const char *src = (kind == 0 ? a.q + t * a.q_step : kind == 1 ? a.k + t * a.k_step : a.v + t * a.v_step) + h * D * 2;
-            float x[8], y[8];
-            u32x4 raw = {0u, 0u, 0u, 0u};
-            if (ok) raw = *(const u32x4 *)(src + e * 2);
-            widen8<ACT>(raw, x);
-            const float *w = kind == 0 ? a.q_weight : a.k_weight;
-            const bool norm = kind < 2 && w != nullptr;
-            float inv = 1.f;
-            float sum = 0.f;
+        // heads of one kind, GH at a time, this wave's share of them: first, first + parts, ...; put(h, bytes from the head's row, y)
+        auto turn_heads = [&](const char *src, int heads, int groups, int before, const float *weight, auto &&put) {
+            int hg = part - before % a.parts;
+            if (hg < 0) hg += a.parts;
+            if (hg >= groups) return;
+            float cw[8], sw[8];
 #pragma unroll
-            for (int i = 0; i < 8; i++) sum = fmaf(x[i], x[i], sum);
-            sum = group_sum<LPH>(sum);
-            if (norm) inv = 1.f / sqrtf(sum * (1.f / D) + a.eps);
-            if (kind < 2 && ok) {
-                float xo[8];
-                if (!turns || in_lane) {
+            for (int i = 0; i < 8; i++) {
+                cw[i] = cs[i];
+                sw[i] = sn[i];
+            }
+            if (weight) {
+                float w[8], wo[8];
+                load_weight8<true>(weight, mine, w);
+                if (PAIRS == 0) {
 #pragma unroll
-                    for (int i = 0; i < 8; i++) xo[i] = x[i ^ 1];
-                } else if (aligned) {
-                    widen8<ACT>(*(const u32x4 *)(src + other[0] * 2), xo);
+                    for (int i = 0; i < 8; i++) wo[i] = w[i ^ 1];
                 } else {
-#pragma unroll
-                    for (int i = 0; i < 8; i++) xo[i] = widen16<ACT>(*(const unsigned short *)(src + other[i] * 2));
+                    load_weight8<PAIRS == 1>(weight, other, wo);
                 }
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
-                    const float mine = norm ? x[i] * inv * w[e + i] : x[i];
-                    const float its = norm ? xo[i] * inv * w[other[i]] : xo[i];
-                    y[i] = e + i < a.rotary ? fmaf(mine, cs[i], its * sn[i]) : mine;
+                    cw[i] *= w[i];
+                    sw[i] *= wo[i];
                 }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; i++) y[i] = x[i];
             }
-            if (CACHE == S3_ROT_MXFP4 ? hh < heads : ok) {  // (a block's four lanes stay together: D is a multiple of 32)
-                if (kind == 0) *(u32x4 *)(a.q_out + t * a.q_out_step + (h * D + e) * 2) = round8<ACT>(y);
-                else if (CACHE == S3_ROT_NONE) *(u32x4 *)(a.k_out + t * a.k_out_step + (h * D + e) * 2) = round8<ACT>(y);
-                else if (CACHE == S3_ROT_16BIT && kind == 2) *(u32x4 *)(a.vplane + row + (h * D + e) * 2) = raw;
-                else store_row8<ACT, D, CACHE>((kind == 1 ? a.kplane : a.vplane) + row, a.Hkv, h, e, y);
+            u32x4 raw, raw_other = {0u, 0u, 0u, 0u};
+            unsigned short one[8];
+            auto load = [&](int group) {
+                const char *at = src + (int64_t)group * (GH * D * 2);
+                const bool ok = lane_ok && group * GH + sub < heads;
+                raw = (u32x4){0u, 0u, 0u, 0u};
+                if (ok) {
+                    raw = *(const u32x4 *)(at + lane_at);
+                    if (PAIRS == 1) raw_other = *(const u32x4 *)(at + other_at);
+                    if (PAIRS == 2) {
+#pragma unroll
+                        for (int i = 0; i < 8; i++) one[i] = *(const unsigned short *)(at + (unsigned)(sub * D + other[i]) * 2);
+                    }
+                }
+            };
+            load(hg);
+            while (true) {
+                float x[8], xo[8], y[8];
+                widen8<ACT>(raw, x);
+                if (PAIRS == 1) widen8<ACT>(raw_other, xo);
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    if (PAIRS == 0) xo[i] = x[i ^ 1];
+                    if (PAIRS == 2) xo[i] = widen16<ACT>(one[i]);
+                }
+                const int h = hg * GH + sub;
+                hg += a.parts;
+                const bool more = hg < groups;
+                if (more) load(hg);  // the next heads are on their way while these are turned
+                float inv = 1.f;
+                if (weight) {
+                    float sum = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 8; i++) sum = fmaf(x[i], x[i], sum);
+                    sum = group_sum<LPH>(sum);
+                    inv = 1.f / sqrtf(sum * (1.f / D) + a.eps);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    // (elements that do not turn: infinities times a sine of 0 are kept out)
+                    const float its = (PAIRS == 1 ? e : e + i) < a.rotary ? xo[i] * inv * sw[i] : 0.f;
+                    y[i] = fmaf(x[i] * inv, cw[i], its);
+                }
+                if (lane_ok && h < heads) put(h, y);
+                if (!more) break;
+            }
+        };
+        turn_heads(a.q + t * a.q_step, a.Hq, gq, 0, a.q_weight, [&](int h, const float (&y)[8]) {
+            *(u32x4 *)(a.q_out + t * a.q_out_step + (h * D + e) * 2) = round8<ACT>(y);
+        });
+        turn_heads(a.k + t * a.k_step, a.Hkv, gk, gq, a.k_weight, [&](int h, const float (&y)[8]) {
+            if (CACHE == S3_ROT_NONE) *(u32x4 *)(a.k_out + t * a.k_out_step + (h * D + e) * 2) = round8<ACT>(y);
+            else store_row8<ACT, D, CACHE>(a.kplane + row, a.Hkv, h, e, y);
+        });
+        if (CACHE != S3_ROT_NONE) {
+            int hg = part - (gq + gk) % a.parts;
+            for (hg = hg < 0 ? hg + a.parts : hg; hg < gk; hg += a.parts) {
+                const int h = hg * GH + sub;
+                if (!lane_ok || h >= a.Hkv) continue;
+                const u32x4 raw = *(const u32x4 *)(a.v + t * a.v_step + (int64_t)hg * (GH * D * 2) + lane_at);
+                if (CACHE == S3_ROT_16BIT) {
+                    *(u32x4 *)(a.vplane + row + (h * D + e) * 2) = raw;
+                } else {
+                    float x[8];
+                    widen8<ACT>(raw, x);
+                    store_row8<ACT, D, CACHE>(a.vplane + row, a.Hkv, h, e, x);
+                }
             }
         }
     }
 }
 
 typedef void (*rotary_fn)(const RotaryArgs);
-template <int ACT, int D>
-static rotary_fn pick_rotary(int cache) {
-    if (cache == S3_ROT_16BIT) return rotary_kernel<ACT, D, S3_ROT_16BIT>;
-    if (cache == S3_ROT_NONE) return rotary_kernel<ACT, D, S3_ROT_NONE>;
+template <int ACT, int D, int PAIRS>
+static rotary_fn pick_cache(int cache) {
+    if (cache == S3_ROT_16BIT) return rotary_kernel<ACT, D, S3_ROT_16BIT, PAIRS>;
+    if (cache == S3_ROT_NONE) return rotary_kernel<ACT, D, S3_ROT_NONE, PAIRS>;
     if constexpr (D != 96) {
-        if (cache == S3_ROT_E4M3) return rotary_kernel<ACT, D, S3_ROT_E4M3>;
-        if (cache == S3_ROT_MXFP4) return rotary_kernel<ACT, D, S3_ROT_MXFP4>;
+        if (cache == S3_ROT_E4M3) return rotary_kernel<ACT, D, S3_ROT_E4M3, PAIRS>;
+        if (cache == S3_ROT_MXFP4) return rotary_kernel<ACT, D, S3_ROT_MXFP4, PAIRS>;
     }
     return nullptr;
 }
-template <int ACT>
-static rotary_fn pick_rotary(int d, int cache) {
-    return d == 64 ? pick_rotary<ACT, 64>(cache) : d == 96 ? pick_rotary<ACT, 96>(cache) : d == 128 ? pick_rotary<ACT, 128>(cache)
-         : d == 256 ? pick_rotary<ACT, 256>(cache) : nullptr;
+template <int ACT, int D>
+static rotary_fn pick_pairs(int cache, int pairs) {
+    return pairs == 0 ? pick_cache<ACT, D, 0>(cache) : pairs == 1 ? pick_cache<ACT, D, 1>(cache) : pick_cache<ACT, D, 2>(cache);
 }
-
-static bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+template <int ACT>
+static rotary_fn pick_rotary(int d, int cache, int pairs) {
+    return d == 64 ? pick_pairs<ACT, 64>(cache, pairs) : d == 96 ? pick_pairs<ACT, 96>(cache, pairs) : d == 128 ? pick_pairs<ACT, 128>(cache, pairs)
+         : d == 256 ? pick_pairs<ACT, 256>(cache, pairs) : nullptr;
+}
 
 // Checks the rule for heads of d elements and puts it into the arguments.
 static bool take_rule(const s3_rotary *r, int d, RotaryArgs &a) {
@@ -211,7 +289,7 @@ static bool take_rule(const s3_rotary *r, int d, RotaryArgs &a) {
     if (r->interleaved != 0 && r->interleaved != 1) return false;
     if (r->rotary_dim > 0 && !r->inv_freq) return false;
     if (r->n_axes > 1 && r->rotary_dim > 0 && !r->axis_of_pair) return false;
-    if ((r->q_weight || r->k_weight) && !(r->eps >= 0.f)) return false;
+    if ((r->q_weight || r->k_weight) && (!(r->eps >= 0.f) || !aligned16(r->q_weight) || !aligned16(r->k_weight))) return false;
     a.rotary = r->rotary_dim;
     a.interleaved = r->interleaved;
     a.n_axes = r->n_axes;
@@ -235,9 +313,10 @@ static int64_t step_bytes(int64_t stride, int heads, int d) {
 }
 
 static int launch_rotary(RotaryArgs &a, int act, int d, int cache, int cus, void *stream) {
-    rotary_fn fn = act == S3_F16 ? pick_rotary<S3_F16>(d, cache) : act == S3_BF16 ? pick_rotary<S3_BF16>(d, cache) : nullptr;
+    const int pairs = a.interleaved || a.rotary == 0 ? 0 : a.rotary % 16 == 0 ? 1 : 2;
+    rotary_fn fn = act == S3_F16 ? pick_rotary<S3_F16>(d, cache, pairs) : act == S3_BF16 ? pick_rotary<S3_BF16>(d, cache, pairs) : nullptr;
     if (!fn) return S3_ERR_INVALID;
-    const int gh = d == 96 ? 4 : 512 / d, groups = (a.Hq + a.Hkv * (cache == S3_ROT_NONE ? 1 : 2) + gh - 1) / gh;
+    const int gh = d == 96 ? 4 : 512 / d, groups = (a.Hq + gh - 1) / gh + (a.Hkv + gh - 1) / gh * (cache == S3_ROT_NONE ? 1 : 2);
     // Few tokens: their heads are shared out over waves until there are some sixteen waves a compute unit, so that a launch is one
     // pass through memory deep; beyond, a wave keeps its token's angles for all of its heads.
     const int64_t waves = (int64_t)16 * cus;
@@ -329,39 +408,42 @@ struct FetchArgs {
     int32_t n, elems, max_len;  // elems: of a row
 };
 
-// A thread: eight elements of a row.
+// A thread: eight elements of a row, the same ones of every row it takes; a workgroup has as many rows at once as it has threads for.
 template <int ACT, int CACHE>
 __global__ void __launch_bounds__(256) fetch_kernel(const FetchArgs a) {
     const char *plane = blockIdx.y ? a.vplane : a.kplane;
     char *out = blockIdx.y ? a.v_out : a.k_out;
     if (!out) return;
-    const int pieces = a.elems / 8;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)a.n * pieces; i += (int64_t)gridDim.x * 256) {
-        const int64_t t = i / pieces;
-        const int e = (int)(i - t * pieces) * 8;
+    const int pieces = a.elems / 8, rows = pieces < 256 ? 256 / pieces : 1;
+    const int mine = threadIdx.x / pieces, first = (threadIdx.x - mine * pieces) * 8;
+    if (mine >= rows) return;
+    for (int64_t t = (int64_t)blockIdx.x * rows + mine; t < a.n; t += (int64_t)gridDim.x * rows) {
         const int64_t off = a.slot_off[t], p = a.pos[t];
         if (off < 0 || p < 0 || p >= a.max_len || off + p >= a.n_tokens) continue;  // never leave the arena
         const char *row = plane + (off + p) * a.row_bytes;
-        u32x4 w;
-        if (CACHE == S3_ROT_16BIT) {
-            w = *(const u32x4 *)(row + e * 2);
-        } else if (CACHE == S3_ROT_E4M3) {
-            const u32x2 c = *(const u32x2 *)(row + e);
-            float lo[4], hi[4];
-            widen4_e4m3(c[0], lo);
-            widen4_e4m3(c[1], hi);
-            const float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            w = round8<ACT>(x);  // (exact: four significant bits)
-        } else {
-            const unsigned c = *(const unsigned *)(row + e / 2);
-            const float scale = fp4_scale(*(const unsigned char *)(row + a.elems / 2 + e / 32));
-            const bf16x2 b[4] = {fp4_widen2<0>(c, scale), fp4_widen2<1>(c, scale), fp4_widen2<2>(c, scale), fp4_widen2<3>(c, scale)};
-            float x[8];
+        char *dst = out + t * a.elems * 2;
+        for (int e = first; e < a.elems; e += 2048) {
+            u32x4 w;
+            if (CACHE == S3_ROT_16BIT) {
+                w = *(const u32x4 *)(row + e * 2);
+            } else if (CACHE == S3_ROT_E4M3) {
+                const u32x2 c = *(const u32x2 *)(row + e);
+                float lo[4], hi[4];
+                widen4_e4m3(c[0], lo);
+                widen4_e4m3(c[1], hi);
+                const float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                w = round8<ACT>(x);  // (exact: four significant bits)
+            } else {
+                const unsigned c = *(const unsigned *)(row + e / 2);
+                const float scale = fp4_scale(*(const unsigned char *)(row + a.elems / 2 + e / 32));
+                const bf16x2 b[4] = {fp4_widen2<0>(c, scale), fp4_widen2<1>(c, scale), fp4_widen2<2>(c, scale), fp4_widen2<3>(c, scale)};
+                float x[8];
 #pragma unroll
-            for (int j = 0; j < 8; j++) x[j] = (float)b[j >> 1][j & 1];
-            w = round8<ACT>(x);  // (exact but for powers of two that the type does not reach)
+                for (int j = 0; j < 8; j++) x[j] = (float)b[j >> 1][j & 1];
+                w = round8<ACT>(x);  // (exact but for powers of two that the type does not reach)
+            }
+            *(u32x4 *)(dst + e * 2) = w;
         }
-        *(u32x4 *)(out + (t * a.elems + e) * 2) = w;
     }
 }
 
@@ -389,7 +471,8 @@ extern "C" int s3_kv_fetch(s3_arena *ar, int32_t layer, int32_t n, const int64_t
     a.elems = ar->cfg.n_kv_heads * ar->cfg.head_dim;
     a.max_len = ar->cfg.max_len;
     const int64_t cus = ar->num_cus > 0 ? ar->num_cus : 256;
-    int64_t blocks = ((int64_t)n * (a.elems / 8) + 255) / 256;
+    const int rows = a.elems / 8 < 256 ? 256 / (a.elems / 8) : 1;
+    int64_t blocks = ((int64_t)n + rows - 1) / rows;
     if (blocks > 16 * cus) blocks = 16 * cus;
     fetch_fn fn = ar->cfg.act_dtype == S3_F16 ? pick_fetch<S3_F16>(ar->cfg.kv_dtype) : pick_fetch<S3_BF16>(ar->cfg.kv_dtype);
     hipLaunchKernelGGL(fn, dim3((unsigned)blocks, 2), dim3(256), 0, (hipStream_t)stream, a);

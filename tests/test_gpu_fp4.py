@@ -390,8 +390,8 @@ def test_static_step_and_replayed_graphs():
 
 
 def test_static_step_that_needs_more_than_the_fixed_scratch():
-    rig = Rig(64, 64, 256, 1, [1] * 200, max_len=16384)
-    n = 200
+    n = 600  # a slot of 64 heads x 258 floats a context and more: beyond 32 MiB
+    rig = Rig(64, 64, 256, 1, [1] * n, max_len=16384)
     q = torch.zeros((n, 64, 256), dtype=torch.bfloat16, device=DEV)
     out = torch.zeros_like(q)
     assert s3.s3_decode_step_static(rig.a, 0, n, rig.off_d, rig.lens_d([0] * n), q, q, q, out, 1) == s3.S3_ERR_SCRATCH
