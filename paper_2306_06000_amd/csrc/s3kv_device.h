@@ -997,9 +997,9 @@ typedef void (*append_fp8_fn)(char *, char *, const int64_t *, const int32_t *, 
                               int64_t, int32_t);
 append_fp8_fn s3i_pick_append_fp8(int act);
 // Kernels for rows of 4-bit blocks (defined in s3kv_fp4.hip): attention for new rows and queries of type act (256 threads; wide_out:
-// 32-bit outputs; heads_per_unit: 2 for pairs of heads of 64; shares: equal shares of all rows, or chunks of contexts; query_bytes: LDS
-// that the queries take) and the append that rounds a new row.
-attn_fn s3i_pick_fp4(int act, int d, int heads_per_unit, bool wide_out, bool shares, int *query_bytes);
+// 32-bit outputs; heads_per_unit: 2 for pairs of heads of 64; shares: equal shares of all rows, or chunks of contexts; lds: bytes of it behind
+// the batch view) and the append that rounds a new row.
+attn_fn s3i_pick_fp4(int act, int d, int heads_per_unit, bool wide_out, bool shares, int *lds);
 append_fp8_fn s3i_pick_append_fp4(int act);
 // Matrix-core kernel for shared key/value heads (defined in s3kv_gqa_mfma.hip): q of type act, rows of the same or (kv8) e4m3
 // codes; 256 threads per workgroup, one work item per wave, or (wide) 512, one per workgroup; loop: more items than waves.

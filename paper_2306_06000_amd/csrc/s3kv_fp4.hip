@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(256) append_fp4_kernel(char *kplane, char *vpl
     for (int i = codes + row_elems / 32 + threadIdx.x; i < row; i += 256) dst[i] = 0;
 }
 
-// A tile of 32 rows of a unit of W elements as a lane loads it.
+// A tile of 32 rows of a unit of W elements as the matrix cores take it from a lane.
 template <int W>
 struct Fp4Tile {
     static constexpr int T = W / 128;
@@ -54,38 +54,98 @@ struct Fp4Tile {
     unsigned vs[8];
 };
 
-// Where a lane's pieces of a tile are, in bytes from its first row.
-struct Fp4Offsets {
-    unsigned k[2], ks[2], v[8], vs[8];
+// Tiles on their way.  Rows go from memory straight into LDS (global_load_lds: lane l's bytes land behind lane l-1's), sixteen bytes a
+// lane with the lanes of a row next to each other: 64 or 128 bytes of a row are one or two cache lines' worth of a load, where loads
+// in operand order (lanes of a quad on four rows) kept the address unit busy for 42 cycles each and the kernel at half its rate.  A
+// wave has its own ring of tiles and waits by the number of loads issued behind the one it needs (they complete in order), so no
+// wave waits for another.
+//   K   row R at R * W/2, its 16-byte pieces exchanged by XOR with R / 4 (256: R / 2), so that the sixteen rows a read takes one piece
+//       of lie in different banks
+//   V   row 16u + 4g + j at row place 16u + 4j + g: the rows that a read takes words of together are neighbours
+//   S   the rows' scale bytes, K then V
+template <int W>
+struct Fp4Ring {
+    static constexpr int T = W / 128, ROW = W / 2, LOADS = 2 * T, PER_LOAD = 32 / LOADS;  // loads of a tile and plane, rows of one
+    static constexpr int STAGE = 2 * 32 * ROW + 64 * 4 * T, TILE_LOADS = 2 * LOADS + T;
+    static constexpr int DEEP = W == 256 ? 2 : 3;  // tiles of a ring of attn_fp4_share_kernel (at most 3: see its waits)
 };
+typedef __attribute__((address_space(3))) void lds_void;
+typedef const __attribute__((address_space(1))) void glb_void;
 
-// Rows of one plane from `base` on, `rows` of them; what lies past them reads as zeros and costs no traffic (a scale of 0 under codes
-// of 0: no NaN comes from there).
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(const char *base, int rows, int row_bytes) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, max(rows, 0) * row_bytes, 0x00020000);
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-template <int W>
-__device__ __forceinline__ void load_tile(Fp4Tile<W> &t, const char *kbase, const char *vbase, int rows, int row_bytes, const Fp4Offsets &o) {
-    constexpr int T = W / 128;
-    const __amdgpu_buffer_rsrc_t kr = rows_from(kbase, rows, row_bytes), vr = rows_from(vbase, rows, row_bytes);
-#pragma unroll
-    for (int u = 0; u < 2; u++)
-#pragma unroll
-        for (int h = 0; h < T; h++) {
-            t.k[u][h] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kr, o.k[u] + 64 * h, 0, 2));
-            t.ks[u][h] = __builtin_amdgcn_raw_buffer_load_b8(kr, o.ks[u] + 4 * h, 0, 0);
-        }
+// A tile out of LDS.  The reads and their wait are one block of machine code: to the compiler, every read of LDS would depend on all
+// loads into it that are in flight.
+__device__ __forceinline__ void read_tile(Fp4Tile<128> &t, unsigned k, unsigned ks, unsigned v, unsigned vs) {
+    asm volatile(
+        "ds_read_b128 %0, %20\n\t"
+        "ds_read_b128 %1, %20 offset:1024\n\t"
+        "ds_read_u8 %2, %21\n\t"
+        "ds_read_u8 %3, %21 offset:64\n\t"
+        "ds_read_b32 %4, %22\n\t"
+        "ds_read_b32 %5, %22 offset:256\n\t"
+        "ds_read_b32 %6, %22 offset:512\n\t"
+        "ds_read_b32 %7, %22 offset:768\n\t"
+        "ds_read_b32 %8, %22 offset:1024\n\t"
+        "ds_read_b32 %9, %22 offset:1280\n\t"
+        "ds_read_b32 %10, %22 offset:1536\n\t"
+        "ds_read_b32 %11, %22 offset:1792\n\t"
+        "ds_read_u8 %12, %23\n\t"
+        "ds_read_u8 %13, %23 offset:4\n\t"
+        "ds_read_u8 %14, %23 offset:8\n\t"
+        "ds_read_u8 %15, %23 offset:12\n\t"
+        "ds_read_u8 %16, %23 offset:64\n\t"
+        "ds_read_u8 %17, %23 offset:68\n\t"
+        "ds_read_u8 %18, %23 offset:72\n\t"
+        "ds_read_u8 %19, %23 offset:76\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(t.k[0][0]), "=&v"(t.k[1][0]), "=&v"(t.ks[0][0]), "=&v"(t.ks[1][0]), "=&v"(t.v[0][0]), "=&v"(t.v[1][0]), "=&v"(t.v[2][0]),
+          "=&v"(t.v[3][0]), "=&v"(t.v[4][0]), "=&v"(t.v[5][0]), "=&v"(t.v[6][0]), "=&v"(t.v[7][0]), "=&v"(t.vs[0]), "=&v"(t.vs[1]),
+          "=&v"(t.vs[2]), "=&v"(t.vs[3]), "=&v"(t.vs[4]), "=&v"(t.vs[5]), "=&v"(t.vs[6]), "=&v"(t.vs[7])
+        : "v"(k), "v"(ks), "v"(v), "v"(vs)
+        : "memory");
+}
+__device__ __forceinline__ void read_tile(Fp4Tile<256> &t, unsigned k, unsigned k2, unsigned ks, unsigned v, unsigned vs) {
+    u32x2 w[8];
+    asm volatile(
+        "ds_read_b128 %0, %24\n\t"
+        "ds_read_b128 %1, %25\n\t"
+        "ds_read_b128 %2, %24 offset:2048\n\t"
+        "ds_read_b128 %3, %25 offset:2048\n\t"
+        "ds_read_u8 %4, %26\n\t"
+        "ds_read_u8 %5, %26 offset:4\n\t"
+        "ds_read_u8 %6, %26 offset:128\n\t"
+        "ds_read_u8 %7, %26 offset:132\n\t"
+        "ds_read_b64 %8, %27\n\t"
+        "ds_read_b64 %9, %27 offset:512\n\t"
+        "ds_read_b64 %10, %27 offset:1024\n\t"
+        "ds_read_b64 %11, %27 offset:1536\n\t"
+        "ds_read_b64 %12, %27 offset:2048\n\t"
+        "ds_read_b64 %13, %27 offset:2560\n\t"
+        "ds_read_b64 %14, %27 offset:3072\n\t"
+        "ds_read_b64 %15, %27 offset:3584\n\t"
+        "ds_read_u8 %16, %28\n\t"
+        "ds_read_u8 %17, %28 offset:8\n\t"
+        "ds_read_u8 %18, %28 offset:16\n\t"
+        "ds_read_u8 %19, %28 offset:24\n\t"
+        "ds_read_u8 %20, %28 offset:128\n\t"
+        "ds_read_u8 %21, %28 offset:136\n\t"
+        "ds_read_u8 %22, %28 offset:144\n\t"
+        "ds_read_u8 %23, %28 offset:152\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(t.k[0][0]), "=&v"(t.k[0][1]), "=&v"(t.k[1][0]), "=&v"(t.k[1][1]), "=&v"(t.ks[0][0]), "=&v"(t.ks[0][1]), "=&v"(t.ks[1][0]),
+          "=&v"(t.ks[1][1]), "=&v"(w[0]), "=&v"(w[1]), "=&v"(w[2]), "=&v"(w[3]), "=&v"(w[4]), "=&v"(w[5]), "=&v"(w[6]), "=&v"(w[7]),
+          "=&v"(t.vs[0]), "=&v"(t.vs[1]), "=&v"(t.vs[2]), "=&v"(t.vs[3]), "=&v"(t.vs[4]), "=&v"(t.vs[5]), "=&v"(t.vs[6]), "=&v"(t.vs[7])
+        : "v"(k), "v"(k2), "v"(ks), "v"(v), "v"(vs)
+        : "memory");
 #pragma unroll
     for (int e = 0; e < 8; e++) {
-        if constexpr (W == 256) {
-            const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(vr, o.v[e], 0, 2));
-            t.v[e][0] = w[0];
-            t.v[e][1] = w[1];
-        } else {
-            t.v[e][0] = __builtin_amdgcn_raw_buffer_load_b32(vr, o.v[e], 0, 2);
-        }
-        t.vs[e] = __builtin_amdgcn_raw_buffer_load_b8(vr, o.vs[e], 0, 0);
+        const unsigned x = w[e][0], y = w[e][1];
+        t.v[e][0] = x;
+        t.v[e][1] = y;
     }
 }
 
@@ -134,10 +194,11 @@ struct Fp4Wave {
     static constexpr int W = D == 256 ? 256 : 128, T = W / 128;
     static constexpr int QP = ACT == S3_F16 ? 2 : 1;  // bf16 parts of a query
     static constexpr int QB = 16 / NH;                // columns of a head
-    static constexpr int Q_BYTES = QP * T * 4 * 1024;  // of the queries in LDS
+    typedef Fp4Ring<W> Ring;
 
     const AttnArgs &a;
-    char *q_lds;  // the queries, as the B operand takes them: [part][half][word][lane]
+    char *ring;  // this wave's tiles on their way
+    bf16x8 q[QP][T][4];
     int lane, r, g;
     int code_bytes, row_bytes;
     int kh0, qb, per_head;  // first cached head, block of query heads, query heads of a cached head in it
@@ -145,11 +206,10 @@ struct Fp4Wave {
     int ksub, vsub, qsub, kblk, vel, khead, vhead, qhead;
     int ko, kso, vo, vso;
     bool column, q_here;
-    Fp4Offsets at_row;
     float m, l;
     f32x4 acc[8 * T];
 
-    __device__ __forceinline__ Fp4Wave(const AttnArgs &args, char *lds) : a(args), q_lds(lds) {
+    __device__ __forceinline__ Fp4Wave(const AttnArgs &args, char *tiles) : a(args), ring(tiles) {
         lane = threadIdx.x & 63;
         r = lane & 15;
         g = lane >> 4;
@@ -178,20 +238,57 @@ struct Fp4Wave {
         qhead = (kh0 + qsub) * a.group + qi;
         column = qi < a.group && (NH == 1 || qsub == 0 || second);
         q_here = column && (D != 64 || (NH == 2 ? ksub == qsub : g < 2));
+    }
+
+    // Issues the loads of a tile that begins at row `row` of the arena and of which `rows` rows (1 and more) are there; rows past them
+    // repeat the last one, whose values they then carry into the products with a weight of 0.
+    __device__ __forceinline__ void issue(char *stage, int64_t row, int rows) const {
+        const char *kp = a.kplane + row * row_bytes, *vp = a.vplane + row * row_bytes;
+        const int last = min(rows, 32) - 1;
+        constexpr int LPR = 64 / Ring::PER_LOAD;  // lanes a row
+        const int base = kh0 * (D / 2), piece = lane % LPR;
+        // (heads that are not there: pieces of the one that is)
+        const int keep = D != 64 || second ? LPR - 1 : 1;
 #pragma unroll
-        for (int u = 0; u < 2; u++) {
-            at_row.k[u] = (16 * u + r) * row_bytes + ko;
-            at_row.ks[u] = (16 * u + r) * row_bytes + kso;
+        for (int i = 0; i < Ring::LOADS; i++) {
+            const int place = i * Ring::PER_LOAD + lane / LPR;
+            const int swap = W == 256 ? (place >> 1) & 7 : (place >> 2) & 3;
+            const unsigned at = min(place, last) * row_bytes + base + ((piece ^ swap) & keep) * 16;
+            __builtin_amdgcn_global_load_lds((glb_void *)(kp + at), (lds_void *)(stage + i * 1024), 16, 0, 2);
         }
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-            const int row = (e & 3) + 4 * g + 16 * (e >> 2);
-            at_row.v[e] = row * row_bytes + vo;
-            at_row.vs[e] = row * row_bytes + vso;
+        for (int i = 0; i < Ring::LOADS; i++) {
+            const int place = i * Ring::PER_LOAD + lane / LPR;
+            const int mine = (place & 16) + 4 * (place & 3) + ((place >> 2) & 3);
+            const unsigned at = min(mine, last) * row_bytes + base + (piece & keep) * 16;
+            __builtin_amdgcn_global_load_lds((glb_void *)(vp + at), (lds_void *)(stage + 32 * Ring::ROW + i * 1024), 16, 0, 2);
+        }
+        const int scales = code_bytes + (kh0 * (D / 32) & ~3);
+        char *s = stage + 64 * Ring::ROW;
+        if (W == 256) {
+            const unsigned at = min(lane >> 1, last) * row_bytes + scales + (lane & 1) * 4;
+            __builtin_amdgcn_global_load_lds((glb_void *)(kp + at), (lds_void *)s, 4, 0, 0);
+            __builtin_amdgcn_global_load_lds((glb_void *)(vp + at), (lds_void *)(s + 256), 4, 0, 0);
+        } else {
+            const unsigned at = min(lane & 31, last) * row_bytes + scales;
+            __builtin_amdgcn_global_load_lds((glb_void *)((lane < 32 ? kp : vp) + at), (lds_void *)s, 4, 0, 0);
+        }
+    }
+    __device__ __forceinline__ void read(Fp4Tile<W> &t, const char *stage) const {
+        const unsigned base = (unsigned)(uintptr_t)(lds_void *)stage, s = base + 64 * Ring::ROW;
+        const int shift = D == 64 && NH == 1 ? 2 * (kh0 & 1) : 0;  // (a unit's scales within their word)
+        const unsigned ks = s + r * 4 * T + shift + (D == 64 && (NH == 1 || !second) ? g & 1 : g);
+        const unsigned v = base + 32 * Ring::ROW + g * Ring::ROW + r * 4 * T;
+        const unsigned vs = s + 128 * T + g * 16 * T + (W == 256 ? r >> 1 : shift + (D == 64 && (NH == 1 || !second) ? (r >> 2) & 1 : r >> 2));
+        if constexpr (W == 256) {
+            const unsigned k = base + r * 128 + ((g ^ ((r >> 1) & 7)) * 16), k2 = base + r * 128 + (((4 + g) ^ ((r >> 1) & 7)) * 16);
+            read_tile(t, k, k2, ks, v, vs);
+        } else {
+            read_tile(t, base + r * 64 + ((g ^ (r >> 2)) * 16), ks, v, vs);
         }
     }
 
-    // Sequence b's queries into LDS (fp16: two exact bf16 parts); nothing folded in yet.
+    // Sequence b's queries (fp16: two exact bf16 parts each); nothing folded in yet.
     __device__ __forceinline__ void begin(int b) {
         u32x4 w[T][4];
 #pragma unroll
@@ -206,7 +303,7 @@ struct Fp4Wave {
 #pragma unroll
             for (int i = 0; i < 4; i++) {
                 if (QP == 1) {
-                    put_query(0, h, i, w[h][i]);
+                    q[0][h][i] = __builtin_bit_cast(bf16x8, w[h][i]);
                 } else {
                     float x[8];
                     widen8<ACT>(w[h][i], x);
@@ -215,7 +312,7 @@ struct Fp4Wave {
                         u32x4 p;
 #pragma unroll
                         for (int e = 0; e < 4; e++) p[e] = take_bf16_part(x[2 * e], x[2 * e + 1]);
-                        put_query(part, h, i, p);
+                        q[part][h][i] = __builtin_bit_cast(bf16x8, p);
                     }
                 }
             }
@@ -223,16 +320,6 @@ struct Fp4Wave {
         l = 0.f;
 #pragma unroll
         for (int i = 0; i < 8 * T; i++) acc[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
-    }
-    __device__ __forceinline__ void put_query(int part, int h, int i, const u32x4 w) {
-        *(u32x4 *)(q_lds + (((part * T + h) * 4 + i) * 64 + lane) * 16) = w;
-    }
-    __device__ __forceinline__ bf16x8 query(int part, int h, int i) const {
-        return __builtin_bit_cast(bf16x8, *(const u32x4 *)(q_lds + (((part * T + h) * 4 + i) * 64 + lane) * 16));
-    }
-
-    __device__ __forceinline__ void load(Fp4Tile<W> &t, const char *kp, const char *vp, int rows) const {
-        load_tile<W>(t, kp, vp, rows, row_bytes, at_row);
     }
 
     // What a tile holds is folded into (m, l, acc); rows: those of the tile and behind it (fewer than 32: the last tile).
@@ -243,14 +330,11 @@ struct Fp4Wave {
             const float scale[2] = {fp4_scale(t.ks[0][h]), fp4_scale(t.ks[1][h])};
 #pragma unroll
             for (int i = 0; i < 4; i++) {
-                bf16x8 q[QP];
-#pragma unroll
-                for (int part = 0; part < QP; part++) q[part] = query(part, h, i);
 #pragma unroll
                 for (int u = 0; u < 2; u++) {
                     const bf16x8 k8 = widen_word(t.k[u][h][i], scale[u]);
 #pragma unroll
-                    for (int part = 0; part < QP; part++) s[u] = mfma_bf16(k8, q[part], s[u]);
+                    for (int part = 0; part < QP; part++) s[u] = mfma_bf16(k8, q[part][h][i], s[u]);
                 }
             }
         }
@@ -266,7 +350,7 @@ struct Fp4Wave {
                     for (int i = 0; i < 4; i++) {
                         const bf16x8 k8 = widen_word(ksub == sub ? t.k[u][0][i] : 0u, ksub == sub ? fp4_scale(t.ks[u][0]) : 1.f);
 #pragma unroll
-                        for (int part = 0; part < QP; part++) c[sub] = mfma_bf16(k8, query(part, 0, i), c[sub]);
+                        for (int part = 0; part < QP; part++) c[sub] = mfma_bf16(k8, q[part][0][i], c[sub]);
                     }
                 }
                 s[u] = qsub ? c[1] : c[0];
@@ -422,17 +506,18 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_team_kernel(const AttnArgs a)
     typedef Fp4Wave<ACT, D, NH, NP> Wave;
     constexpr int W = Wave::W, T = Wave::T, QB = Wave::QB, TS = 4;
     constexpr int STRIDE = W + 4;  // floats of a column in LDS
-    extern __shared__ __align__(16) char dyn_lds[];  // the batch view, the queries, then the waves' sums of the columns in use
+    extern __shared__ __align__(16) char dyn_lds[];  // the batch view, the waves' rings
     __shared__ int wave_sums[S3_MAX_CLASSES * S3_MAX_WAVES];
     __shared__ float comb_m[TS][16], comb_l[TS][16];
     __shared__ int last_of_context;
     const int ts = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // (scalar: row ranges and buffers with it)
     const BatchView bv = build_batch_view<false>(a, dyn_lds, wave_sums);
-    char *queries = dyn_lds + ((batch_view_bytes(a.n, a.ncls) + 15) & ~(size_t)15);
-    float *comb = (float *)(queries + Wave::Q_BYTES);
+    char *rings = dyn_lds + ((batch_view_bytes(a.n, a.ncls) + 15) & ~(size_t)15);
+    // a wave's ring takes its sums of the columns in use when its rows are done: STRIDE floats a column
+    constexpr int RING = 2 * Wave::Ring::STAGE;
+    static_assert(16 * STRIDE * 4 <= RING, "a wave's sums fit its ring");
     publish_lengths<D>(a, bv);
-    Wave w(a, queries);  // (the waves have the same queries: each writes all of them, so none waits for another)
-    const int row_bytes = w.row_bytes;
+    Wave w(a, rings + ts * RING);
     // Work in the order of eighths: workgroup b (XCD b % 8) takes the chunks whose number leaves the same remainder, so that the
     // columns of a chunk, whose bytes share cache lines, are on one XCD's L2.
     const int64_t total = (int64_t)((bv.total + 7) / 8) * 8 * a.columns;
@@ -447,22 +532,23 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_team_kernel(const AttnArgs a)
         const int j0 = min(end, start + ts * per), j1 = min(end, j0 + per);
         const bool has_new = a.k_new != nullptr && j1 == it.len && j0 < j1;
         w.set_column(col);
-        const char *kp = a.kplane + (it.off + j0) * (int64_t)row_bytes, *vp = a.vplane + (it.off + j0) * (int64_t)row_bytes;
-        const int64_t step = 32 * (int64_t)row_bytes, new_row = it.off + it.len - 1;
-        // Two tiles' registers in turn, so that the next tile's loads are out while one is folded in.
-        Fp4Tile<W> t0, t1;
-        w.load(t0, kp, vp, j1 - j0);
+        const int64_t first_row = it.off + j0;
+        const int tiles = (j1 - j0 + 31) / 32;
+        // a tile is on its way while the one before it is folded in
+        if (tiles > 0) w.issue(w.ring, first_row, j1 - j0);
         w.begin(it.b);
-        for (int left = j1 - j0; left > 0; left -= 64) {
-            w.load(t1, kp + step, vp + step, left - 32);
-            if (has_new && left <= 32) w.take_new_row(t0, it.b, new_row, left);
-            w.fold(t0, left);
-            if (left <= 32) break;
-            kp += 2 * step;
-            vp += 2 * step;
-            w.load(t0, kp, vp, left - 64);
-            if (has_new && left <= 64) w.take_new_row(t1, it.b, new_row, left - 32);
-            w.fold(t1, left - 32);
+        for (int i = 0; i < tiles; i++) {
+            const int left = j1 - j0 - 32 * i;
+            Fp4Tile<W> t;
+            if (left > 32) {
+                w.issue(w.ring + ((i + 1) & 1) * Wave::Ring::STAGE, first_row + 32 * (i + 1), left - 32);
+                wait_loads<Wave::Ring::TILE_LOADS>();
+            } else {
+                wait_loads<0>();
+            }
+            w.read(t, w.ring + (i & 1) * Wave::Ring::STAGE);
+            if (has_new && left <= 32) w.take_new_row(t, it.b, it.off + it.len - 1, left);
+            w.fold(t, left);
         }
 
         // the four waves meet: columns in use, compact (head, query)
@@ -477,7 +563,7 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_team_kernel(const AttnArgs a)
             for (int rr = 0; rr < 4; rr++)
 #pragma unroll
                 for (int i = 0; i < 2 * T; i++)
-                    *(f32x4 *)(comb + ((size_t)ts * n_cols + slot) * STRIDE + 8 * T * (4 * w.g + rr) + 4 * i) = w.sums4(rr, i);
+                    *(f32x4 *)((float *)w.ring + slot * STRIDE + 8 * T * (4 * w.g + rr) + 4 * i) = w.sums4(rr, i);
         }
         __syncthreads();
         // a thread: eight elements of one column
@@ -493,7 +579,7 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_team_kernel(const AttnArgs a)
             for (int x = 0; x < TS; x++) {
                 const float wt = fast_exp2(comb_m[x][c] - ref);
                 ll += wt * comb_l[x][c];
-                const float *src = comb + ((size_t)x * n_cols + c) * STRIDE + sub * 64 + dl * 8;
+                const float *src = (const float *)(rings + x * RING) + c * STRIDE + sub * 64 + dl * 8;
                 const f32x4 x0 = *(const f32x4 *)src, x1 = *(const f32x4 *)(src + 4);
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
@@ -545,11 +631,11 @@ template <int ACT, int D, int NH, int NP>
 __global__ void __launch_bounds__(256, 2) attn_fp4_share_kernel(const AttnArgs a) {
     typedef Fp4Wave<ACT, D, NH, NP> Wave;
     constexpr int W = Wave::W, T = Wave::T, QB = Wave::QB;
-    extern __shared__ __align__(16) char dyn_lds[];  // the batch view in tiles, then the waves' queries
+    extern __shared__ __align__(16) char dyn_lds[];  // the batch view in tiles, the waves' rings
     __shared__ int wave_sums[3 * S3_MAX_WAVES];
     int longest = 0;
     const BatchView bv = build_tile_view<32>(a, dyn_lds, wave_sums, longest);
-    char *queries = dyn_lds + ((batch_view_bytes(a.n, 1) + 15) & ~(size_t)15);
+    char *rings = dyn_lds + ((batch_view_bytes(a.n, 1) + 15) & ~(size_t)15);
     publish_lengths<D>(a, bv);
     const int ts = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // Neighbouring columns, whose bytes share cache lines, are on neighbouring waves, and those on one XCD (workgroup b is on XCD b % 8).
@@ -568,9 +654,9 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_share_kernel(const AttnArgs a
         if (t0 >= t1) return;
         t1 = __builtin_amdgcn_readfirstlane(bv.pre[find_sequence(bv.pre, a.n, t1 - 1) + 1]);
     }
-    Wave w(a, queries + ts * Wave::Q_BYTES);
+    constexpr int DEEP = Wave::Ring::DEEP;
+    Wave w(a, rings + ts * DEEP * Wave::Ring::STAGE);
     w.set_column(col);
-    const int row_bytes = w.row_bytes;
     Pending head = {0, 0, 0}, tail = {0, 0, 0};  // pieces of the contexts that the share's borders cut
 
     // the loader: context, its first tile, rows from the tile to load on (0: the share is loaded)
@@ -589,10 +675,6 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_share_kernel(const AttnArgs a
         c.len = __builtin_amdgcn_readfirstlane(bv.len[c.b]);
         c.off = uniform64(bv.off[c.b]);
         c.tile = tile;
-    };
-    const auto load = [&](Fp4Tile<W> &t, const Cursor &c, bool there) {
-        const int64_t row = c.off + (int64_t)(c.tile - c.begin) * 32;
-        w.load(t, a.kplane + row * row_bytes, a.vplane + row * row_bytes, there ? c.len - (c.tile - c.begin) * 32 : 0);
     };
     const auto finish = [&](const Cursor &c) {  // the share's part of context c.b is folded in
         const int first = max(c.begin, t0), last = min(c.end, t1);
@@ -627,40 +709,45 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_share_kernel(const AttnArgs a
                 for (int i = 0; i < 2 * T; i++) put_partial4<true>(pa + 8 * T * rr + 4 * i, w.sums4(rr, i));
         }
     };
-    // one tile: the next one's loads leave, then this one is folded in
-    Cursor now;
+    // the loader runs DEEP - 1 tiles ahead, across the contexts' borders
+    Cursor now, ahead;
     now.b = b;
     open(now, t0);
-    const auto advance = [&](const Cursor &c, Fp4Tile<W> &t) {
-        Cursor n = c;
-        const bool there = c.tile + 1 < t1;
-        if (there) {
-            if (c.tile + 1 < c.end) n.tile++;
-            else open(n, c.tile + 1);
-        }
-        load(t, n, there);
-        return n;
+    ahead = now;
+    int put = 0, take = 0;  // places in the ring
+    const auto issue = [&]() {
+        const int begun = (ahead.tile - ahead.begin) * 32;
+        w.issue(w.ring + put * Wave::Ring::STAGE, ahead.off + begun, ahead.len - begun);
+        put = put + 1 == DEEP ? 0 : put + 1;
+        if (ahead.tile + 1 < ahead.end) ahead.tile++;
+        else if (ahead.tile + 1 < t1) open(ahead, ahead.tile + 1);
+        else ahead.tile++;
     };
-    const auto one = [&](Fp4Tile<W> &t, const Cursor &c, int next_b) {
-        const int rows = c.len - (c.tile - c.begin) * 32;
-        if (a.k_new != nullptr && rows <= 32) w.take_new_row(t, c.b, c.off + c.len - 1, rows);
-        w.fold(t, rows);
-        const bool last = c.tile + 1 == t1;
-        if (last || c.tile + 1 == c.end) {
-            finish(c);
-            if (!last) w.begin(next_b);
-        }
-    };
-    Fp4Tile<W> ta, tb;
-    load(ta, now, true);
+#pragma unroll
+    for (int i = 0; i < DEEP - 1; i++)
+        if (ahead.tile < t1) issue();
     w.begin(now.b);
     while (true) {
-        Cursor next = advance(now, tb);
-        one(ta, now, next.b);
-        if (now.tile + 1 >= t1) break;
-        now = advance(next, ta);
-        one(tb, next, now.b);
-        if (next.tile + 1 >= t1) break;
+        Fp4Tile<W> t;
+        if (ahead.tile < t1) issue();
+        const int behind = ahead.tile - 1 - now.tile;  // tiles issued behind the one that is folded in now
+        if (behind >= 2) wait_loads<2 * Wave::Ring::TILE_LOADS>();
+        else if (behind == 1) wait_loads<Wave::Ring::TILE_LOADS>();
+        else wait_loads<0>();
+        w.read(t, w.ring + take * Wave::Ring::STAGE);
+        take = take + 1 == DEEP ? 0 : take + 1;
+        const int rows = now.len - (now.tile - now.begin) * 32;
+        if (a.k_new != nullptr && rows <= 32) w.take_new_row(t, now.b, now.off + now.len - 1, rows);
+        w.fold(t, rows);
+        const int next = now.tile + 1;
+        if (next == now.end || next == t1) {
+            finish(now);
+            if (next == t1) break;
+            open(now, next);
+            w.begin(now.b);
+        } else {
+            now.tile = next;
+        }
     }
     if (head.count + tail.count == 0) return;
     const unsigned who = pieces_arrived(a, head, tail, a.columns, col);
@@ -686,8 +773,9 @@ static attn_fn pick_fp4(int d, int nh) {
     return d == 128 ? attn_fp4_team_kernel<ACT, 128, 1, NP> : d == 256 ? attn_fp4_team_kernel<ACT, 256, 1, NP> : nullptr;
 }
 
-attn_fn s3i_pick_fp4(int act, int d, int heads_per_unit, bool wide_out, bool shares, int *query_bytes) {
-    *query_bytes = (shares ? 4 : 1) * (act == S3_F16 ? 2 : 1) * (d == 256 ? 2 : 1) * 4096;
+attn_fn s3i_pick_fp4(int act, int d, int heads_per_unit, bool wide_out, bool shares, int *lds) {
+    const int stage = d == 256 ? Fp4Ring<256>::STAGE : Fp4Ring<128>::STAGE;
+    *lds = 4 * stage * (shares ? d == 256 ? Fp4Ring<256>::DEEP : Fp4Ring<128>::DEEP : 2);
     if (act == S3_F16) {
         if (wide_out) return shares ? pick_fp4<S3_F16, 3, true>(d, heads_per_unit) : pick_fp4<S3_F16, 3, false>(d, heads_per_unit);
         return shares ? pick_fp4<S3_F16, 2, true>(d, heads_per_unit) : pick_fp4<S3_F16, 2, false>(d, heads_per_unit);

@@ -748,7 +748,7 @@ static size_t chunk_slots(const s3_arena *a, int n, int n_hg, size_t slot_bytes,
 // of 128 or 256, two neighbouring heads of 64 while their query heads fit the sixteen columns together.  A column (of the work
 // list) is a unit and up to sixteen (eight a head) of its query heads.
 struct Fp4Plan {
-    int heads_per_unit, blocks_per_head, columns, used;  // used: matrix columns that carry query heads
+    int heads_per_unit, blocks_per_head, columns;
     bool shares;    // equal shares of all rows, one a wave (attn_fp4_share_kernel), or chunks of contexts, one a workgroup
     int32_t few;    // chunks that few contexts are cut into, 0: chunks of `chunk` rows
     int chunk;
@@ -762,7 +762,6 @@ static Fp4Plan fp4_plan(const s3_arena *a, int n) {
     const int width = 16 / p.heads_per_unit;
     p.blocks_per_head = (group + width - 1) / width;
     p.columns = (Hkv + p.heads_per_unit - 1) / p.heads_per_unit * p.blocks_per_head;
-    p.used = p.heads_per_unit * (group < width ? group : width);
     p.chunk = a->chunk > 0 ? a->chunk : 1024;
     const size_t slot_bytes = (size_t)a->cfg.n_heads * ((size_t)D * sizeof(float) + sizeof(float2));
     const int64_t fixed = (int64_t)((S3_STATIC_SCRATCH_BYTES - counters_bytes(p.columns)) / slot_bytes);
@@ -1023,8 +1022,8 @@ static int launch_fp8(s3_arena *a, const AttnCall &c) {
 static int launch_fp4(s3_arena *a, const AttnCall &c) {
     const int D = a->cfg.head_dim;
     const Fp4Plan p = fp4_plan(a, c.n);
-    int query_bytes = 0;
-    attn_fn fn = s3i_pick_fp4(a->cfg.act_dtype, D, p.heads_per_unit, c.out_dtype == S3_F32, p.shares, &query_bytes);
+    int lds = 0;  // behind the batch view
+    attn_fn fn = s3i_pick_fp4(a->cfg.act_dtype, D, p.heads_per_unit, c.out_dtype == S3_F32, p.shares, &lds);
     if (!fn) return S3_ERR_INVALID;
     AttnArgs args = common_args(a, c, a->cfg.n_kv_heads, a->cfg.n_heads, p.shares ? 32 : p.chunk);
     args.few_chunks = p.few;
@@ -1036,7 +1035,7 @@ static int launch_fp4(s3_arena *a, const AttnCall &c) {
     const int cus = a->num_cus > 0 ? a->num_cus : 256;
     if (p.shares) {
         args.ncls = 1;
-        const size_t dyn_lds = ((batch_view_lds(c.n, 1) + 15) & ~(size_t)15) + query_bytes;
+        const size_t dyn_lds = ((batch_view_lds(c.n, 1) + 15) & ~(size_t)15) + lds;
         int per_cu = 0;
         rc = resident_per_cu((const void *)fn, 256, dyn_lds, &per_cu);
         if (rc != S3_OK) return rc;
@@ -1044,10 +1043,8 @@ static int launch_fp4(s3_arena *a, const AttnCall &c) {
         args.wave_shares = 4 * cus * per_cu / p.columns;
         return launch_attn_kernels(a, fn, cus * per_cu, 256, dyn_lds, c.stream, args, 0, !c.static_scratch);
     }
-    // LDS: the batch view, the queries, and the sums of four waves
-    const size_t more = query_bytes + 4 * (size_t)p.used * ((D == 256 ? 256 : 128) + 4) * sizeof(float);
-    while (args.ncls > 1 && batch_view_lds(c.n, args.ncls) + more > (size_t)144 * 1024) args.ncls--;
-    const size_t dyn_lds = ((batch_view_lds(c.n, args.ncls) + 15) & ~(size_t)15) + more;
+    while (args.ncls > 1 && batch_view_lds(c.n, args.ncls) + lds > (size_t)156 * 1024) args.ncls--;
+    const size_t dyn_lds = ((batch_view_lds(c.n, args.ncls) + 15) & ~(size_t)15) + lds;
     int blocks = 0;
     rc = stride_grid(a, (const void *)fn, 256, dyn_lds, 1, &blocks);
     if (rc != S3_OK) return rc;
