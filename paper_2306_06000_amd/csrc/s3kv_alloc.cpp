@@ -51,17 +51,20 @@ static bool config_ok(const s3_kv_config *c) {
     return true;
 }
 
-// Bytes of one cached row: H*D elements; 4-bit rows: their codes, a scale byte per 32 of them, up to a multiple of 16 bytes.
-static int64_t row_bytes_of(const s3_kv_config *cfg) {
+// Bytes of one cached row: H*D elements; 4-bit rows: their codes, and apart from them (tail) a scale byte per 32, up to a multiple
+// of 16 bytes.
+static int64_t row_bytes_of(const s3_kv_config *cfg, int64_t *tail) {
     const int64_t elems = (int64_t)(cfg->n_kv_heads > 0 ? cfg->n_kv_heads : cfg->n_heads) * cfg->head_dim;
-    if (cfg->kv_dtype == S3_MXFP4) return (elems / 2 + elems / 32 + 15) & ~(int64_t)15;
-    return elems * (cfg->kv_dtype == S3_E4M3 ? 1 : 2);
+    *tail = cfg->kv_dtype == S3_MXFP4 ? (elems / 32 + 15) & ~(int64_t)15 : 0;
+    return cfg->kv_dtype == S3_MXFP4 ? elems / 2 : elems * (cfg->kv_dtype == S3_E4M3 ? 1 : 2);
 }
 
 extern "C" int64_t s3_kv_bytes_per_token(const s3_kv_config *cfg) {
     if (!config_ok(cfg)) return S3_ERR_INVALID;
     // K and V, every layer, H*D two-byte numbers: 4*l*d_h bytes (section 2.1)
-    return (int64_t)2 * cfg->n_layers * row_bytes_of(cfg);
+    int64_t tail = 0;
+    const int64_t row = row_bytes_of(cfg, &tail);
+    return (int64_t)2 * cfg->n_layers * (row + tail);
 }
 
 extern "C" int s3_kv_arena_init(s3_arena **out, const s3_kv_config *cfg, void *dev_base, size_t dev_bytes) {
@@ -74,7 +77,7 @@ extern "C" int s3_kv_arena_init(s3_arena **out, const s3_kv_config *cfg, void *d
     a->dev_bytes = dev_bytes;
     if (a->cfg.n_kv_heads == 0) a->cfg.n_kv_heads = cfg->n_heads;
     if (cfg->kv_dtype == S3_F16 || cfg->kv_dtype == S3_BF16) a->cfg.act_dtype = cfg->kv_dtype;
-    a->row_bytes = row_bytes_of(cfg);
+    a->row_bytes = row_bytes_of(cfg, &a->tail_bytes);
     a->n_tokens = (int64_t)(dev_bytes / (size_t)s3_kv_bytes_per_token(cfg));
     a->plane_bytes = a->n_tokens * a->row_bytes;
     if (a->n_tokens > 0) a->free_ext[0] = a->n_tokens;
@@ -204,9 +207,7 @@ extern "C" int s3_kv_grow(s3_arena *a, int32_t slot_id, int32_t len, int64_t *ne
     const int64_t off2 = s3i_carve(a, cap2);  // the old extent is still reserved: no overlap possible
     if (off2 < 0) return S3_ERR_NOMEM;
     if (a->base && len > 0) {
-        const int rc = s3i_launch_copy_planes(a->base + old_off * a->row_bytes, a->base + off2 * a->row_bytes,
-                                              (size_t)len * (size_t)a->row_bytes, (size_t)a->plane_bytes,
-                                              (size_t)a->plane_bytes, 2 * a->cfg.n_layers, stream);
+        const int rc = s3i_launch_move_rows(a, old_off, off2, len, stream);
         if (rc != S3_OK) {
             s3i_release(a, off2, cap2);
             return rc;
@@ -249,10 +250,7 @@ extern "C" int s3_kv_compact(s3_arena *a, int32_t n, const int32_t *slot_id, con
                 // each piece lands on rows that the previous piece has already left
                 for (int64_t r = 0; r < keep; r += gap) {
                     const int64_t piece = keep - r < gap ? keep - r : gap;
-                    const int rc = s3i_launch_copy_planes(
-                        a->base + (s.off + r) * a->row_bytes, a->base + (cursor + r) * a->row_bytes,
-                        (size_t)piece * (size_t)a->row_bytes, (size_t)a->plane_bytes, (size_t)a->plane_bytes,
-                        2 * a->cfg.n_layers, stream);
+                    const int rc = s3i_launch_move_rows(a, s.off + r, cursor + r, piece, stream);
                     if (rc != S3_OK) return rc;  // rows already moved stay moved; the table below is not updated
                 }
             }

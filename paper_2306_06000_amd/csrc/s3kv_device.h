@@ -18,6 +18,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 struct AttnArgs {
     char *kplane;
     char *vplane;
+    char *kscale, *vscale;  // 4-bit rows: planes of their scales
     const char *q;
     const int64_t *slot_off;
     const int32_t *cur_len;  // rows to attend minus len_add
@@ -1000,7 +1001,8 @@ append_fp8_fn s3i_pick_append_fp8(int act);
 // 32-bit outputs; heads_per_unit: 2 for pairs of heads of 64; shares: equal shares of all rows, or chunks of contexts; lds: bytes of it behind
 // the batch view) and the append that rounds a new row.
 attn_fn s3i_pick_fp4(int act, int d, int heads_per_unit, bool wide_out, bool shares, int *lds);
-append_fp8_fn s3i_pick_append_fp4(int act);
+typedef void (*append_fp4_fn)(const AttnArgs);  // kplane .. vscale, slot_off, cur_len, k_new, v_new, n_tokens, H * D in `columns`, max_len
+append_fp4_fn s3i_pick_append_fp4(int act);
 // Matrix-core kernel for shared key/value heads (defined in s3kv_gqa_mfma.hip): q of type act, rows of the same or (kv8) e4m3
 // codes; 256 threads per workgroup, one work item per wave, or (wide) 512, one per workgroup; loop: more items than waves.
 attn_fn s3i_pick_gqa_mfma(int act, int d, bool kv8, bool wide, bool loop);

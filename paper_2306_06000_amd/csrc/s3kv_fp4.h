@@ -1,7 +1,8 @@
 // Cache rows of 4-bit blocks (S3_MXFP4) on gfx950: the open microscaling format of e2m1 codes (1 sign, 2 exponent bits with
 // bias 1, 1 fraction bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6) in blocks of 32 consecutive elements of a head under one power of two,
-// 2^(byte - 127).  A stored row is [H][D/2] bytes of codes (element 2i in the low half of byte i), [H][D/32] scale bytes, and
-// zeros up to a multiple of 16 bytes.
+// 2^(byte - 127).  In the arena a row's codes ([H][D/2] bytes, element 2i in the low half of byte i) and its scales ([H][D/32]
+// bytes, zeros up to a multiple of 16) lie in planes of their own: with both in one row, rows began anywhere in a cache line, every head's
+// wave fetched the line of the row's scales for itself, and half of what was fetched was not used.
 //
 // Rounding a block: the scale is the least power of two under which the largest magnitude is below 7, where the nearest code
 // is 6 at the most, so no element is off by more than half the distance between its neighbours (the next value would be 8).
@@ -14,7 +15,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 __host__ __device__ __forceinline__ int fp4_code_bytes(int heads, int d) { return heads * (d / 2); }
-__host__ __device__ __forceinline__ int fp4_row_bytes(int heads, int d) { return (heads * (d / 2 + d / 32) + 15) & ~15; }
+__host__ __device__ __forceinline__ int fp4_scale_bytes(int heads, int d) { return (heads * (d / 32) + 15) & ~15; }
 
 // Scale byte of a block whose largest magnitude is `most`: its exponent, one more from 1.75 * 2^k up, less 2.
 template <int ACT>

@@ -18,19 +18,18 @@
 // meet through memory as in the other kernels.
 #include "s3kv_fp4.h"
 
-// grid (n, 2): block (b, which) rounds one new row of H*D 16-bit elements into row off+pos; a thread has eight elements.
+// grid (n, 2): block (b, which) rounds one new row of `columns` 16-bit elements into row off+pos; a thread has eight elements.
 template <int ACT>
-__global__ void __launch_bounds__(256) append_fp4_kernel(char *kplane, char *vplane, const int64_t *slot_off, const int32_t *pos,
-                                                         const char *k_new, const char *v_new, int32_t row_elems, int64_t n_tokens,
-                                                         int32_t max_len) {
-    const int b = blockIdx.x;
-    const int64_t off = slot_off[b];
-    const int64_t p = pos[b];
-    if (off < 0 || p < 0 || p >= max_len || off + p >= n_tokens) return;  // never leave the arena
-    const char *src = (blockIdx.y ? v_new : k_new) + (int64_t)b * row_elems * 2;
-    const int codes = row_elems / 2, row = (codes + row_elems / 32 + 15) & ~15;
-    char *dst = (blockIdx.y ? vplane : kplane) + (off + p) * (int64_t)row;
-    for (int i = threadIdx.x; i < row_elems / 8; i += 256) {  // (a block's four threads are neighbours and stay together)
+__global__ void __launch_bounds__(256) append_fp4_kernel(const AttnArgs a) {
+    const int b = blockIdx.x, elems = a.columns;
+    const int64_t off = a.slot_off[b];
+    const int64_t p = a.cur_len[b];
+    if (off < 0 || p < 0 || p >= a.max_len || off + p >= a.n_tokens) return;  // never leave the arena
+    const char *src = (blockIdx.y ? a.v_new : a.k_new) + (int64_t)b * elems * 2;
+    const int scales = elems / 32, scale_row = (scales + 15) & ~15;
+    char *codes = (blockIdx.y ? a.vplane : a.kplane) + (off + p) * (int64_t)(elems / 2);
+    char *scale = (blockIdx.y ? a.vscale : a.kscale) + (off + p) * (int64_t)scale_row;
+    for (int i = threadIdx.x; i < elems / 8; i += 256) {  // (a block's four threads are neighbours and stay together)
         float x[8];
         widen8<ACT>(*(const u32x4 *)(src + (int64_t)i * 16), x);
         unsigned most = 0;
@@ -38,10 +37,10 @@ __global__ void __launch_bounds__(256) append_fp4_kernel(char *kplane, char *vpl
         for (int e = 0; e < 8; e++) most = fp4_magnitude(x[e], most);
         most = group_max<4>(most);
         const unsigned byte = fp4_scale_byte<ACT>(__builtin_bit_cast(float, most));
-        *(unsigned *)(dst + i * 4) = fp4_codes8(x, byte);
-        if ((i & 3) == 0) *(unsigned char *)(dst + codes + i / 4) = (unsigned char)byte;
+        *(unsigned *)(codes + i * 4) = fp4_codes8(x, byte);
+        if ((i & 3) == 0) scale[i / 4] = (char)byte;
     }
-    for (int i = codes + row_elems / 32 + threadIdx.x; i < row; i += 256) dst[i] = 0;
+    for (int i = scales + threadIdx.x; i < scale_row; i += 256) scale[i] = 0;
 }
 
 // A tile of 32 rows of a unit of W elements as the matrix cores take it from a lane.
@@ -200,7 +199,7 @@ struct Fp4Wave {
     char *ring;  // this wave's tiles on their way
     bf16x8 q[QP][T][4];
     int lane, r, g;
-    int code_bytes, row_bytes;
+    int code_bytes, scale_bytes;  // of a row
     int kh0, qb, per_head;  // first cached head, block of query heads, query heads of a cached head in it
     bool second;            // the unit has two heads
     int ksub, vsub, qsub, kblk, vel, khead, vhead, qhead;
@@ -214,7 +213,7 @@ struct Fp4Wave {
         r = lane & 15;
         g = lane >> 4;
         code_bytes = fp4_code_bytes(a.H, D);
-        row_bytes = fp4_row_bytes(a.H, D);
+        scale_bytes = fp4_scale_bytes(a.H, D);
     }
 
     // Which heads: of the A operand's lanes (K: block group g; V: elements of lane m = r), of the B operand's columns.
@@ -231,9 +230,9 @@ struct Fp4Wave {
         kblk = D == 64 ? g & 1 : g;                             // (+ 4 for the second half of 256)
         vel = D == 256 ? 16 * r : D == 64 ? 8 * (r & 7) : 8 * r;  // first element of the V words
         ko = khead * (D / 2) + kblk * 16;
-        kso = code_bytes + khead * (D / 32) + kblk;
+        kso = khead * (D / 32) + kblk;
         vo = vhead * (D / 2) + vel / 2;
-        vso = code_bytes + vhead * (D / 32) + vel / 32;
+        vso = vhead * (D / 32) + vel / 32;
         const int qi = (r % QB) + qb * QB;
         qhead = (kh0 + qsub) * a.group + qi;
         column = qi < a.group && (NH == 1 || qsub == 0 || second);
@@ -243,7 +242,8 @@ struct Fp4Wave {
     // Issues the loads of a tile that begins at row `row` of the arena and of which `rows` rows (1 and more) are there; rows past them
     // repeat the last one, whose values they then carry into the products with a weight of 0.
     __device__ __forceinline__ void issue(char *stage, int64_t row, int rows) const {
-        const char *kp = a.kplane + row * row_bytes, *vp = a.vplane + row * row_bytes;
+        const char *kp = a.kplane + row * code_bytes, *vp = a.vplane + row * code_bytes;
+        const char *ks = a.kscale + row * scale_bytes, *vs = a.vscale + row * scale_bytes;
         const int last = min(rows, 32) - 1;
         constexpr int LPR = 64 / Ring::PER_LOAD;  // lanes a row
         const int base = kh0 * (D / 2), piece = lane % LPR;
@@ -253,25 +253,25 @@ struct Fp4Wave {
         for (int i = 0; i < Ring::LOADS; i++) {
             const int place = i * Ring::PER_LOAD + lane / LPR;
             const int swap = W == 256 ? (place >> 1) & 7 : (place >> 2) & 3;
-            const unsigned at = min(place, last) * row_bytes + base + ((piece ^ swap) & keep) * 16;
+            const unsigned at = min(place, last) * code_bytes + base + ((piece ^ swap) & keep) * 16;
             __builtin_amdgcn_global_load_lds((glb_void *)(kp + at), (lds_void *)(stage + i * 1024), 16, 0, 2);
         }
 #pragma unroll
         for (int i = 0; i < Ring::LOADS; i++) {
             const int place = i * Ring::PER_LOAD + lane / LPR;
             const int mine = (place & 16) + 4 * (place & 3) + ((place >> 2) & 3);
-            const unsigned at = min(mine, last) * row_bytes + base + (piece & keep) * 16;
+            const unsigned at = min(mine, last) * code_bytes + base + (piece & keep) * 16;
             __builtin_amdgcn_global_load_lds((glb_void *)(vp + at), (lds_void *)(stage + 32 * Ring::ROW + i * 1024), 16, 0, 2);
         }
-        const int scales = code_bytes + (kh0 * (D / 32) & ~3);
+        const int scales = kh0 * (D / 32) & ~3;
         char *s = stage + 64 * Ring::ROW;
         if (W == 256) {
-            const unsigned at = min(lane >> 1, last) * row_bytes + scales + (lane & 1) * 4;
-            __builtin_amdgcn_global_load_lds((glb_void *)(kp + at), (lds_void *)s, 4, 0, 0);
-            __builtin_amdgcn_global_load_lds((glb_void *)(vp + at), (lds_void *)(s + 256), 4, 0, 0);
+            const unsigned at = min(lane >> 1, last) * scale_bytes + scales + (lane & 1) * 4;
+            __builtin_amdgcn_global_load_lds((glb_void *)(ks + at), (lds_void *)s, 4, 0, 0);
+            __builtin_amdgcn_global_load_lds((glb_void *)(vs + at), (lds_void *)(s + 256), 4, 0, 0);
         } else {
-            const unsigned at = min(lane & 31, last) * row_bytes + scales;
-            __builtin_amdgcn_global_load_lds((glb_void *)((lane < 32 ? kp : vp) + at), (lds_void *)s, 4, 0, 0);
+            const unsigned at = min(lane & 31, last) * scale_bytes + scales;
+            __builtin_amdgcn_global_load_lds((glb_void *)((lane < 32 ? ks : vs) + at), (lds_void *)s, 4, 0, 0);
         }
     }
     __device__ __forceinline__ void read(Fp4Tile<W> &t, const char *stage) const {
@@ -416,7 +416,7 @@ struct Fp4Wave {
     // A decode step's new row, still 16-bit, as the last of a tile's `rows` rows: its blocks are rounded by the lanes that use them and
     // written to the arena (row `row`) by those that own the bytes.
     __device__ __forceinline__ void take_new_row(Fp4Tile<W> &t, int b, int64_t row, int rows) const {
-        const int64_t at = row * row_bytes;
+        const int64_t at = row * code_bytes, scale_at = row * scale_bytes;
         const bool k_own = r == 0 && (D != 64 || (NH == 2 ? ksub == 0 || second : g < 2));
         const bool v_own = g == 0 && (D != 64 || (NH == 2 ? vsub == 0 || second : r < 8));
         const char *ksrc = a.k_new + (((int64_t)b * a.H + khead) * D + kblk * 32) * 2;
@@ -437,7 +437,7 @@ struct Fp4Wave {
             for (int i = 0; i < 4; i++) c[i] = fp4_codes8(x[i], byte);
             if (k_own) {
                 *(u32x4 *)(a.kplane + at + ko + 64 * h) = c;
-                *(unsigned char *)(a.kplane + at + kso + 4 * h) = (unsigned char)byte;
+                a.kscale[scale_at + kso + 4 * h] = (char)byte;
             }
 #pragma unroll
             for (int u = 0; u < 2; u++)
@@ -464,11 +464,11 @@ struct Fp4Wave {
             for (int e = 0; e < 8; e++)
                 if (16 * (e >> 2) + 4 * g + (e & 3) >= rows - 1) t.v[e][h] = c;
         }
-        if (v_own && vel % 32 == 0) *(unsigned char *)(a.vplane + at + vso) = (unsigned char)byte;
-        const int used = code_bytes + a.H * (D / 32);
-        if (kh0 + NH >= a.H && lane < row_bytes - used) {  // zeros up to a multiple of 16 bytes
-            a.kplane[at + used + lane] = 0;
-            a.vplane[at + used + lane] = 0;
+        if (v_own && vel % 32 == 0) a.vscale[scale_at + vso] = (char)byte;
+        const int used = a.H * (D / 32);
+        if (kh0 + NH >= a.H && lane < scale_bytes - used) {  // zeros up to a multiple of 16 bytes
+            a.kscale[scale_at + used + lane] = 0;
+            a.vscale[scale_at + used + lane] = 0;
         }
 #pragma unroll
         for (int e = 0; e < 8; e++)
@@ -784,6 +784,6 @@ attn_fn s3i_pick_fp4(int act, int d, int heads_per_unit, bool wide_out, bool sha
     return shares ? pick_fp4<S3_BF16, 2, true>(d, heads_per_unit) : pick_fp4<S3_BF16, 2, false>(d, heads_per_unit);
 }
 
-append_fp8_fn s3i_pick_append_fp4(int act) {
+append_fp4_fn s3i_pick_append_fp4(int act) {
     return act == S3_F16 ? append_fp4_kernel<S3_F16> : act == S3_BF16 ? append_fp4_kernel<S3_BF16> : nullptr;
 }

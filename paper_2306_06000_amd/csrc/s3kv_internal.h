@@ -19,8 +19,9 @@ struct s3_arena {
     char *base = nullptr;      // device memory owned by the caller (nullptr: metadata only)
     size_t dev_bytes = 0;
     int64_t n_tokens = 0;      // N: token rows the arena holds
-    int64_t row_bytes = 0;     // kv heads * D elements (4-bit rows: with their scales, up to a multiple of 16)
-    int64_t plane_bytes = 0;   // N * row_bytes; plane p = 2*layer + (0: K, 1: V)
+    int64_t row_bytes = 0;     // kv heads * D elements (4-bit rows: their codes)
+    int64_t tail_bytes = 0;    // 4-bit rows: their scale bytes, up to a multiple of 16; else 0
+    int64_t plane_bytes = 0;   // N * row_bytes; plane p = 2*layer + (0: K, 1: V).  Behind the planes: those of the tails, N * tail_bytes each
 
     std::map<int64_t, int64_t> free_ext;  // offset -> size, disjoint, coalesced
     std::vector<s3_slot> slots;           // indexed by id
@@ -56,6 +57,14 @@ struct s3_arena {
     char *plane(int32_t layer, int32_t which) const {
         return base + (int64_t)(2 * layer + which) * plane_bytes;
     }
+    char *tails(int32_t layer, int32_t which) const {  // scale bytes of 4-bit rows
+        return part(1) + (int64_t)(2 * layer + which) * n_tokens * tail_bytes;
+    }
+    // What is copied when rows move: the planes, and the tails' planes behind them.
+    int parts() const { return tail_bytes > 0 ? 2 : 1; }
+    char *part(int i) const { return i ? base + (int64_t)2 * cfg.n_layers * plane_bytes : base; }
+    int64_t part_row(int i) const { return i ? tail_bytes : row_bytes; }
+    int64_t stored_bytes() const { return row_bytes + tail_bytes; }  // a row as s3_kv_fill takes it
 };
 
 // host bookkeeping (s3kv_alloc.cpp)
@@ -68,6 +77,7 @@ void s3i_set_hip_error(const char *what, int code, const char *text);
 // device work (s3kv_kernels.hip); each returns an s3_status
 int s3i_launch_copy_planes(const char *src, char *dst, size_t nbytes, size_t src_plane_stride,
                            size_t dst_plane_stride, int planes, void *stream);
+int s3i_launch_move_rows(const s3_arena *a, int64_t from, int64_t to, int64_t rows, void *stream);  // in every plane
 int s3i_num_variants();    // kernel variants of the multi-head attention kernels
 int s3i_default_variant(); // the one an arena uses unless told otherwise
 int s3i_num_gqa_shapes();  // shapes of the shared-K/V (grouped-query) attention kernel

@@ -5,7 +5,8 @@
 // rows) and s3kv_fp4.hip (rows of 4-bit blocks) and are launched from here; the device helpers all of them share are in s3kv_device.h.
 //
 // Arena layout.  Plane p = 2*layer + (0: K, 1: V) holds N token rows of H*D elements (H = cached
-// heads), token-major: element (token t, head h, d) of a plane sits at ((t*H + h)*D + d).  A slot
+// heads), token-major: element (token t, head h, d) of a plane sits at ((t*H + h)*D + d).  (Rows of 4-bit blocks: planes of
+// codes, and behind them all planes of scales, see s3kv_fp4.h.)  A slot
 // is the row range [off, off+cap) in EVERY plane, so one sequence's rows of one plane are one
 // contiguous run and the attention kernels stream them with 128-bit loads.
 #include <hip/hip_ext.h>
@@ -142,6 +143,58 @@ __global__ void __launch_bounds__(256) fill_batch_kernel(const FillArgs f, int64
     }
 }
 
+// 4-bit rows between the caller's form (a row's codes, then its scales) and the arena's (planes of codes, planes of scales): grid (x, 2,
+// entries), blockIdx.z picks the run of rows, blockIdx.y K or V, a workgroup takes one row at a time.
+struct SplitArgs {
+    char *rows[2][S3_FILL_MAX];    // K, V: the caller's rows
+    char *codes[2][S3_FILL_MAX], *scales[2][S3_FILL_MAX];  // in the arena, from the run's first row on
+    int64_t off[S3_FILL_MAX];
+    int32_t n[S3_FILL_MAX], idx[S3_FILL_MAX];
+    int32_t code16, scale16;       // 16-byte pieces of a row
+};
+template <bool JOIN>
+__global__ void __launch_bounds__(256) split_rows_kernel(const SplitArgs f, int64_t *slot_off, int32_t *len) {
+    const int z = blockIdx.z, row16 = f.code16 + f.scale16;
+    u32x4 *rows = (u32x4 *)f.rows[blockIdx.y][z], *codes = (u32x4 *)f.codes[blockIdx.y][z], *scales = (u32x4 *)f.scales[blockIdx.y][z];
+    const int at_once = row16 < 256 ? 256 / row16 : 1, mine = threadIdx.x / row16, first = threadIdx.x - mine * row16;
+    if (mine < at_once) {
+        for (int64_t r = (int64_t)blockIdx.x * at_once + mine; r < f.n[z]; r += (int64_t)gridDim.x * at_once) {
+            for (int i = first; i < row16; i += 256) {
+                u32x4 *in = rows + r * row16 + i, *at = i < f.code16 ? codes + r * f.code16 + i : scales + r * f.scale16 + (i - f.code16);
+                if (JOIN) *in = *at;
+                else *at = __builtin_nontemporal_load(in);
+            }
+        }
+    }
+    if (slot_off && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
+        slot_off[f.idx[z]] = f.off[z];
+        len[f.idx[z]] = f.n[z];
+    }
+}
+
+// `count` runs of rows (at most S3_FILL_MAX): `f` holds the callers' rows, off (first row of the arena), n and idx.
+static int launch_split_rows(const s3_arena *a, int32_t layer, SplitArgs &f, int count, int which, bool join, int64_t *slot_off, int32_t *len,
+                             void *stream) {
+    f.code16 = (int32_t)(a->row_bytes / 16);
+    f.scale16 = (int32_t)(a->tail_bytes / 16);
+    int64_t most = 1;
+    for (int i = 0; i < count; i++) {
+        for (int w = 0; w < 2; w++) {
+            const int plane = which < 0 ? w : which;
+            f.codes[w][i] = a->plane(layer, plane) + f.off[i] * a->row_bytes;
+            f.scales[w][i] = a->tails(layer, plane) + f.off[i] * a->tail_bytes;
+        }
+        if (f.n[i] > most) most = f.n[i];
+    }
+    const int row16 = f.code16 + f.scale16, at_once = row16 < 256 ? 256 / row16 : 1;
+    const int64_t blocks = (most + at_once - 1) / at_once, limit = 16384 / (2 * count);
+    const dim3 grid((unsigned)(blocks < limit ? blocks : limit), which < 0 ? 2 : 1, (unsigned)count);
+    if (join) hipLaunchKernelGGL(split_rows_kernel<true>, grid, dim3(256), 0, (hipStream_t)stream, f, slot_off, len);
+    else hipLaunchKernelGGL(split_rows_kernel<false>, grid, dim3(256), 0, (hipStream_t)stream, f, slot_off, len);
+    HIP_TRY(hipGetLastError());
+    return S3_OK;
+}
+
 extern "C" int s3_kv_fill_batch(s3_arena *a, int32_t layer, int32_t n_new, const int32_t *slot_id, const int32_t *n_rows,
                                 const void *const *k_rows, const void *const *v_rows, int32_t batch_n,
                                 int64_t *slot_off, int32_t *len, const int32_t *batch_idx, void *stream) {
@@ -158,7 +211,21 @@ extern "C" int s3_kv_fill_batch(s3_arena *a, int32_t layer, int32_t n_new, const
             return S3_ERR_INVALID;
         if (patch && (batch_idx[i] < 0 || batch_idx[i] >= batch_n)) return S3_ERR_INVALID;
     }
-    for (int32_t first = 0; first < n_new; first += S3_FILL_MAX) {
+    for (int32_t first = 0; first < n_new && a->tail_bytes > 0; first += S3_FILL_MAX) {
+        SplitArgs f;
+        memset(&f, 0, sizeof(f));
+        const int count = n_new - first < S3_FILL_MAX ? n_new - first : S3_FILL_MAX;
+        for (int i = 0; i < count; i++) {
+            f.rows[0][i] = (char *)k_rows[first + i];
+            f.rows[1][i] = (char *)v_rows[first + i];
+            f.off[i] = s3i_live_slot(a, slot_id[first + i])->off;
+            f.n[i] = n_rows[first + i];
+            f.idx[i] = patch ? batch_idx[first + i] : 0;
+        }
+        const int rc = launch_split_rows(a, layer, f, count, -1, false, patch ? slot_off : nullptr, patch ? len : nullptr, stream);
+        if (rc != S3_OK) return rc;
+    }
+    for (int32_t first = 0; first < n_new && a->tail_bytes == 0; first += S3_FILL_MAX) {
         FillArgs f;
         memset(&f, 0, sizeof(f));
         const int count = n_new - first < S3_FILL_MAX ? n_new - first : S3_FILL_MAX;
@@ -200,6 +267,16 @@ int s3i_launch_copy_planes(const char *src, char *dst, size_t nbytes, size_t src
     hipLaunchKernelGGL(copy_planes_kernel, dim3((unsigned)blocks, (unsigned)planes), dim3(256), 0,
                        (hipStream_t)stream, src, dst, n16, src_plane_stride, dst_plane_stride);
     HIP_TRY(hipGetLastError());
+    return S3_OK;
+}
+
+int s3i_launch_move_rows(const s3_arena *a, int64_t from, int64_t to, int64_t rows, void *stream) {
+    for (int i = 0; i < a->parts(); i++) {
+        const int64_t row = a->part_row(i);
+        const int rc = s3i_launch_copy_planes(a->part(i) + from * row, a->part(i) + to * row, (size_t)(rows * row),
+                                              (size_t)(a->n_tokens * row), (size_t)(a->n_tokens * row), 2 * a->cfg.n_layers, stream);
+        if (rc != S3_OK) return rc;
+    }
     return S3_OK;
 }
 
@@ -456,11 +533,22 @@ static int launch_append(s3_arena *a, int32_t layer, int32_t n, const int64_t *s
                            a->plane(layer, 1), slot_off, pos, (const char *)k_new, (const char *)v_new,
                            (int32_t)a->row_bytes, a->n_tokens, a->cfg.max_len);
     } else if (a->cfg.kv_dtype == S3_MXFP4) {
-        append_fp8_fn fn = s3i_pick_append_fp4(a->cfg.act_dtype);
+        append_fp4_fn fn = s3i_pick_append_fp4(a->cfg.act_dtype);
         if (!fn) return S3_ERR_INVALID;
-        hipLaunchKernelGGL(fn, dim3((unsigned)n, 2), dim3(256), 0, (hipStream_t)stream, a->plane(layer, 0),
-                           a->plane(layer, 1), slot_off, pos, (const char *)k_new, (const char *)v_new,
-                           (int32_t)(a->cfg.n_kv_heads * a->cfg.head_dim), a->n_tokens, a->cfg.max_len);
+        AttnArgs args;
+        memset(&args, 0, sizeof(args));
+        args.kplane = a->plane(layer, 0);
+        args.vplane = a->plane(layer, 1);
+        args.kscale = a->tails(layer, 0);
+        args.vscale = a->tails(layer, 1);
+        args.slot_off = slot_off;
+        args.cur_len = pos;
+        args.k_new = (const char *)k_new;
+        args.v_new = (const char *)v_new;
+        args.columns = a->cfg.n_kv_heads * a->cfg.head_dim;
+        args.n_tokens = a->n_tokens;
+        args.max_len = a->cfg.max_len;
+        hipLaunchKernelGGL(fn, dim3((unsigned)n, 2), dim3(256), 0, (hipStream_t)stream, args);
     } else {
         hipLaunchKernelGGL(append_kernel, dim3((unsigned)n, 2), dim3(256), 0, (hipStream_t)stream, a->plane(layer, 0),
                            a->plane(layer, 1), slot_off, pos, (const char *)k_new, (const char *)v_new, a->row_bytes,
@@ -537,6 +625,10 @@ static AttnArgs common_args(const s3_arena *a, const AttnCall &c, int row_heads,
     memset(&args, 0, sizeof(args));
     args.kplane = a->plane(c.layer, 0);
     args.vplane = a->plane(c.layer, 1);
+    if (a->tail_bytes > 0) {
+        args.kscale = a->tails(c.layer, 0);
+        args.vscale = a->tails(c.layer, 1);
+    }
     args.q = (const char *)c.q;
     args.k_new = (const char *)c.k_new;
     args.v_new = (const char *)c.v_new;
@@ -1149,6 +1241,15 @@ extern "C" int s3_kv_fill(s3_arena *a, int32_t slot_id, int32_t layer, int32_t f
     const size_t nbytes = (size_t)n_rows * a->row_bytes;
     const int64_t row0 = s->off + first_row;
     if (((uintptr_t)k_rows & 15) || ((uintptr_t)v_rows & 15)) return S3_ERR_INVALID;
+    if (a->tail_bytes > 0) {
+        SplitArgs f;
+        memset(&f, 0, sizeof(f));
+        f.rows[0][0] = (char *)k_rows;
+        f.rows[1][0] = (char *)v_rows;
+        f.off[0] = row0;
+        f.n[0] = n_rows;
+        return launch_split_rows(a, layer, f, 1, -1, false, nullptr, nullptr, stream);
+    }
     const size_t n16 = nbytes / 16;
     size_t blocks = (n16 + S3_FILL_U * 256 - 1) / (S3_FILL_U * 256);
     if (blocks > 4096) blocks = 4096;
@@ -1162,18 +1263,20 @@ extern "C" int s3_kv_fill(s3_arena *a, int32_t slot_id, int32_t layer, int32_t f
 // ---- evict to / restore from host memory (the paper's own misprediction path, section 3 and 4.3) ----
 extern "C" int64_t s3_kv_evict_bytes(const s3_arena *a, int32_t len) {
     if (!a || len < 0 || len > a->cfg.max_len) return S3_ERR_INVALID;
-    return (int64_t)2 * a->cfg.n_layers * len * a->row_bytes;
+    return (int64_t)2 * a->cfg.n_layers * len * a->stored_bytes();
 }
 
 extern "C" int s3_kv_evict(s3_arena *a, int32_t slot_id, int32_t len, void *host_buf, void *stream) {
     const s3_slot *s = s3i_live_slot(a, slot_id);
     if (!s || !a->base || len < 0 || len > s->cap || (len > 0 && !host_buf)) return S3_ERR_INVALID;
-    const size_t piece = (size_t)len * (size_t)a->row_bytes;
     const int planes = 2 * a->cfg.n_layers;
-    for (int p = 0; p < planes && piece; p++)
-        HIP_TRY(hipMemcpyAsync((char *)host_buf + (size_t)p * piece,
-                               a->base + (int64_t)p * a->plane_bytes + s->off * a->row_bytes, piece,
-                               hipMemcpyDeviceToHost, (hipStream_t)stream));
+    char *to = (char *)host_buf;
+    for (int i = 0; i < a->parts(); i++) {
+        const size_t piece = (size_t)len * (size_t)a->part_row(i);
+        for (int p = 0; p < planes && piece; p++, to += piece)
+            HIP_TRY(hipMemcpyAsync(to, a->part(i) + ((int64_t)p * a->n_tokens + s->off) * a->part_row(i), piece, hipMemcpyDeviceToHost,
+                                   (hipStream_t)stream));
+    }
     return s3_kv_free(a, slot_id);
 }
 
@@ -1186,15 +1289,17 @@ extern "C" int s3_kv_restore(s3_arena *a, int32_t predicted_len, int32_t len, co
     const int admitted = s3_kv_alloc(a, 1, &predicted_len, &id, &off, &cap);
     if (admitted < 0) return admitted;
     if (admitted == 0) return S3_ERR_NOMEM;
-    const size_t piece = (size_t)len * (size_t)a->row_bytes;
     const int planes = 2 * a->cfg.n_layers;
-    for (int p = 0; p < planes && piece; p++) {
-        const hipError_t e = hipMemcpyAsync(a->base + (int64_t)p * a->plane_bytes + off * a->row_bytes,
-                                            (const char *)host_buf + (size_t)p * piece, piece, hipMemcpyHostToDevice,
-                                            (hipStream_t)stream);
-        if (e != hipSuccess) {
-            (void)s3_kv_free(a, id);
-            return hip_fail("hipMemcpyAsync(restore)", e);
+    const char *from = (const char *)host_buf;
+    for (int i = 0; i < a->parts(); i++) {
+        const size_t piece = (size_t)len * (size_t)a->part_row(i);
+        for (int p = 0; p < planes && piece; p++, from += piece) {
+            const hipError_t e = hipMemcpyAsync(a->part(i) + ((int64_t)p * a->n_tokens + off) * a->part_row(i), from, piece,
+                                                hipMemcpyHostToDevice, (hipStream_t)stream);
+            if (e != hipSuccess) {
+                (void)s3_kv_free(a, id);
+                return hip_fail("hipMemcpyAsync(restore)", e);
+            }
         }
     }
     *slot_id = id;
@@ -1209,17 +1314,29 @@ extern "C" int s3_kv_restore(s3_arena *a, int32_t predicted_len, int32_t len, co
 extern "C" int s3_kv_gather_rows(s3_arena *a, int32_t slot_id, int32_t len, void *dev_buf, void *stream) {
     const s3_slot *s = s3i_live_slot(a, slot_id);
     if (!s || !a->base || len < 0 || len > s->cap || (len > 0 && (!dev_buf || ((uintptr_t)dev_buf & 15)))) return S3_ERR_INVALID;
-    const size_t piece = (size_t)len * (size_t)a->row_bytes;
-    return s3i_launch_copy_planes(a->base + s->off * a->row_bytes, (char *)dev_buf, piece, (size_t)a->plane_bytes, piece,
-                                  2 * a->cfg.n_layers, stream);
+    char *to = (char *)dev_buf;
+    for (int i = 0; i < a->parts(); i++) {
+        const int64_t row = a->part_row(i);
+        const size_t piece = (size_t)len * (size_t)row;
+        const int rc = s3i_launch_copy_planes(a->part(i) + s->off * row, to, piece, (size_t)(a->n_tokens * row), piece, 2 * a->cfg.n_layers, stream);
+        if (rc != S3_OK) return rc;
+        to += (size_t)2 * a->cfg.n_layers * piece;
+    }
+    return S3_OK;
 }
 
 extern "C" int s3_kv_scatter_rows(s3_arena *a, int32_t slot_id, int32_t len, const void *dev_buf, void *stream) {
     const s3_slot *s = s3i_live_slot(a, slot_id);
     if (!s || !a->base || len < 0 || len > s->cap || (len > 0 && (!dev_buf || ((uintptr_t)dev_buf & 15)))) return S3_ERR_INVALID;
-    const size_t piece = (size_t)len * (size_t)a->row_bytes;
-    return s3i_launch_copy_planes((const char *)dev_buf, a->base + s->off * a->row_bytes, piece, piece, (size_t)a->plane_bytes,
-                                  2 * a->cfg.n_layers, stream);
+    const char *from = (const char *)dev_buf;
+    for (int i = 0; i < a->parts(); i++) {
+        const int64_t row = a->part_row(i);
+        const size_t piece = (size_t)len * (size_t)row;
+        const int rc = s3i_launch_copy_planes(from, a->part(i) + s->off * row, piece, piece, (size_t)(a->n_tokens * row), 2 * a->cfg.n_layers, stream);
+        if (rc != S3_OK) return rc;
+        from += (size_t)2 * a->cfg.n_layers * piece;
+    }
+    return S3_OK;
 }
 
 // A copy that deliberately occupies few compute units, and occupies them alone: `workgroups` workgroups of 1024
@@ -1275,6 +1392,15 @@ extern "C" int s3_kv_read_rows(s3_arena *a, int32_t slot_id, int32_t layer, int3
     if ((int64_t)first_row + n_rows > s->cap) return S3_ERR_INVALID;
     if (n_rows == 0) return S3_OK;
     if (!dst) return S3_ERR_INVALID;
+    if (a->tail_bytes > 0) {
+        if ((uintptr_t)dst & 15) return S3_ERR_INVALID;
+        SplitArgs f;
+        memset(&f, 0, sizeof(f));
+        f.rows[0][0] = (char *)dst;
+        f.off[0] = s->off + first_row;
+        f.n[0] = n_rows;
+        return launch_split_rows(a, layer, f, 1, which, true, nullptr, nullptr, stream);
+    }
     return s3i_launch_copy_planes(a->plane(layer, which) + (s->off + first_row) * a->row_bytes, (char *)dst,
                                   (size_t)n_rows * a->row_bytes, 0, 0, 1, stream);
 }

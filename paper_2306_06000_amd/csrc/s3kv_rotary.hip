@@ -24,7 +24,7 @@ struct RotaryArgs {
     const char *q, *k, *v;
     char *q_out, *k_out;
     int64_t q_step, k_step, v_step, q_out_step, k_out_step;  // bytes from token to token
-    char *kplane, *vplane;
+    char *kplane, *vplane, *kscale, *vscale;
     const int64_t *slot_off;
     const int32_t *pos, *rot_pos;  // rot_pos: [n_axes][n], null: pos on every axis
     const float *inv_freq, *q_weight, *k_weight;
@@ -68,9 +68,9 @@ __device__ __forceinline__ u32x4 round8(const float (&y)[8]) {
     return w;
 }
 
-// Eight elements (from element e of head h, x in fp32; raw: as they came, if they are a bit copy) of a row at `row` into the cache.
+// Eight elements (from element e of head h, x in fp32) of a row of the cache, its codes or numbers at `row`, 4-bit: its scales at `scale`.
 template <int ACT, int D, int CACHE>
-__device__ __forceinline__ void store_row8(char *row, int heads, int h, int e, const float (&x)[8]) {
+__device__ __forceinline__ void store_row8(char *row, char *scale, int heads, int h, int e, const float (&x)[8]) {
     if (CACHE == S3_ROT_16BIT) {
         *(u32x4 *)(row + (h * D + e) * 2) = round8<ACT>(x);
     } else if (CACHE == S3_ROT_E4M3) {
@@ -84,11 +84,10 @@ __device__ __forceinline__ void store_row8(char *row, int heads, int h, int e, c
         for (int i = 0; i < 8; i++) most = fp4_magnitude(x[i], most);
         most = group_max<4>(most);
         const unsigned byte = fp4_scale_byte<ACT>(__builtin_bit_cast(float, most));
-        const int codes = fp4_code_bytes(heads, D);
         *(unsigned *)(row + (h * D + e) / 2) = fp4_codes8(x, byte);
-        if ((e & 31) == 0) *(unsigned char *)(row + codes + (h * D + e) / 32) = (unsigned char)byte;
+        if ((e & 31) == 0) scale[(h * D + e) / 32] = (char)byte;
         if (h == heads - 1 && e == D - 8)  // zeros up to a multiple of 16 bytes
-            for (int i = codes + heads * (D / 32); i < fp4_row_bytes(heads, D); i++) row[i] = 0;
+            for (int i = heads * (D / 32); i < fp4_scale_bytes(heads, D); i++) scale[i] = 0;
     }
 }
 
@@ -117,7 +116,7 @@ __global__ void __launch_bounds__(256) rotary_kernel(const RotaryArgs a) {
     const int lane = threadIdx.x & 63, sub = lane / LPH, e0 = (lane % LPH) * 8;
     const bool lane_ok = D != 96 || e0 < D;
     const int e = lane_ok ? e0 : 0;
-    const int64_t row_bytes = CACHE == S3_ROT_MXFP4 ? fp4_row_bytes(a.Hkv, D) : (int64_t)a.Hkv * D * (CACHE == S3_ROT_E4M3 ? 1 : 2);
+    const int64_t row_bytes = CACHE == S3_ROT_MXFP4 ? fp4_code_bytes(a.Hkv, D) : (int64_t)a.Hkv * D * (CACHE == S3_ROT_E4M3 ? 1 : 2);
     const int half = a.rotary / 2;
     // this lane's elements: turns per position, axis and other element of the pair, whatever the token
     double rate[8];
@@ -141,13 +140,14 @@ __global__ void __launch_bounds__(256) rotary_kernel(const RotaryArgs a) {
     for (int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); item < (int64_t)a.n * a.parts; item += (int64_t)gridDim.x * 4) {
         const int64_t t = uniform64(a.parts == 1 ? item : item / a.parts);
         const int part = __builtin_amdgcn_readfirstlane((int)(item - t * a.parts));
-        int64_t row = 0;
+        int64_t row = 0, scale = 0;  // bytes into the planes
         int32_t p = 0;
         if (CACHE != S3_ROT_NONE) {
             const int64_t off = a.slot_off[t];
             p = a.pos[t];
             if (off < 0 || p < 0 || p >= a.max_len || off + p >= a.n_tokens) continue;  // never leave the arena
             row = (off + p) * row_bytes;
+            scale = CACHE == S3_ROT_MXFP4 ? (off + p) * fp4_scale_bytes(a.Hkv, D) : 0;
         }
         float cs[8], sn[8];
         {
@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(256) rotary_kernel(const RotaryArgs a) {
         });
         turn_heads(a.k + t * a.k_step, a.Hkv, gk, gq, a.k_weight, [&](int h, const float (&y)[8]) {
             if (CACHE == S3_ROT_NONE) *(u32x4 *)(a.k_out + t * a.k_out_step + (h * D + e) * 2) = round8<ACT>(y);
-            else store_row8<ACT, D, CACHE>(a.kplane + row, a.Hkv, h, e, y);
+            else store_row8<ACT, D, CACHE>(a.kplane + row, a.kscale + scale, a.Hkv, h, e, y);
         });
         if (CACHE != S3_ROT_NONE) {
             int hg = part - (gq + gk) % a.parts;
@@ -255,7 +255,7 @@ __global__ void __launch_bounds__(256) rotary_kernel(const RotaryArgs a) {
                 } else {
                     float x[8];
                     widen8<ACT>(raw, x);
-                    store_row8<ACT, D, CACHE>(a.vplane + row, a.Hkv, h, e, x);
+                    store_row8<ACT, D, CACHE>(a.vplane + row, a.vscale + scale, a.Hkv, h, e, x);
                 }
             }
         }
@@ -388,6 +388,10 @@ extern "C" int s3_kv_append_rotary(s3_arena *ar, int32_t layer, int32_t n, const
     a.q_out = (char *)q_out;
     a.kplane = ar->plane(layer, 0);
     a.vplane = ar->plane(layer, 1);
+    if (ar->tail_bytes > 0) {
+        a.kscale = ar->tails(layer, 0);
+        a.vscale = ar->tails(layer, 1);
+    }
     a.slot_off = slot_off;
     a.pos = pos;
     a.rot_pos = rot_pos;
@@ -400,11 +404,11 @@ extern "C" int s3_kv_append_rotary(s3_arena *ar, int32_t layer, int32_t n, const
 
 // ---- cached rows as numbers ----------------------------------------------------------------------------------------
 struct FetchArgs {
-    const char *kplane, *vplane;
+    const char *kplane, *vplane, *kscale, *vscale;
     const int64_t *slot_off;
     const int32_t *pos;
     char *k_out, *v_out;
-    int64_t n_tokens, row_bytes;
+    int64_t n_tokens, row_bytes, scale_bytes;
     int32_t n, elems, max_len;  // elems: of a row
 };
 
@@ -420,7 +424,7 @@ __global__ void __launch_bounds__(256) fetch_kernel(const FetchArgs a) {
     for (int64_t t = (int64_t)blockIdx.x * rows + mine; t < a.n; t += (int64_t)gridDim.x * rows) {
         const int64_t off = a.slot_off[t], p = a.pos[t];
         if (off < 0 || p < 0 || p >= a.max_len || off + p >= a.n_tokens) continue;  // never leave the arena
-        const char *row = plane + (off + p) * a.row_bytes;
+        const char *row = plane + (off + p) * a.row_bytes, *scales = (blockIdx.y ? a.vscale : a.kscale) + (off + p) * a.scale_bytes;
         char *dst = out + t * a.elems * 2;
         for (int e = first; e < a.elems; e += 2048) {
             u32x4 w;
@@ -435,7 +439,7 @@ __global__ void __launch_bounds__(256) fetch_kernel(const FetchArgs a) {
                 w = round8<ACT>(x);  // (exact: four significant bits)
             } else {
                 const unsigned c = *(const unsigned *)(row + e / 2);
-                const float scale = fp4_scale(*(const unsigned char *)(row + a.elems / 2 + e / 32));
+                const float scale = fp4_scale(*(const unsigned char *)(scales + e / 32));
                 const bf16x2 b[4] = {fp4_widen2<0>(c, scale), fp4_widen2<1>(c, scale), fp4_widen2<2>(c, scale), fp4_widen2<3>(c, scale)};
                 float x[8];
 #pragma unroll
@@ -467,6 +471,9 @@ extern "C" int s3_kv_fetch(s3_arena *ar, int32_t layer, int32_t n, const int64_t
     a.v_out = (char *)v_out;
     a.n_tokens = ar->n_tokens;
     a.row_bytes = ar->row_bytes;
+    a.scale_bytes = ar->tail_bytes;
+    a.kscale = ar->tail_bytes > 0 ? ar->tails(layer, 0) : nullptr;
+    a.vscale = ar->tail_bytes > 0 ? ar->tails(layer, 1) : nullptr;
     a.n = n;
     a.elems = ar->cfg.n_kv_heads * ar->cfg.head_dim;
     a.max_len = ar->cfg.max_len;

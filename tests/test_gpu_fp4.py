@@ -32,7 +32,7 @@ class Rig:
     """An arena with one slot a sequence, in an order other than the batch's."""
 
     def __init__(self, heads, kv, d, act, preds, max_len=2048, granule=64, layers=1, seed=0, spare=0):
-        self.heads, self.kv, self.d, self.act = heads, kv, d, act
+        self.heads, self.kv, self.d, self.act, self.layers = heads, kv, d, act, layers
         self.rng = np.random.default_rng([seed, heads, kv, d, act])
         self.cfg = s3.make_config(layers, heads, d, s3.S3_MXFP4, granule, max_len, 0 if kv == heads else kv, act)
         bpt = s3.s3_kv_bytes_per_token(self.cfg)
@@ -65,6 +65,13 @@ class Rig:
         dst = torch.empty((rows, self.row), dtype=torch.uint8, device=DEV)
         assert s3.s3_kv_read_rows(self.a, int(self.ids[i]), layer, which, 0, rows, dst, self.stream) == 0
         return dst.cpu().numpy()
+
+    def rows(self, mem=None):
+        """The arena as stored rows [layers][2][N][row]: codes and scales lie in planes of their own."""
+        m = (self.mem if mem is None else mem)[:2 * self.layers * self.N * self.row]
+        codes = self.kv * self.d // 2
+        cut = 2 * self.layers * self.N * codes
+        return torch.cat([m[:cut].view(self.layers, 2, self.N, codes), m[cut:].view(self.layers, 2, self.N, self.row - codes)], -1)
 
     def lens_d(self, lens):
         return torch.tensor(lens, dtype=torch.int32, device=DEV)
@@ -174,8 +181,8 @@ def test_append_rounds_bit_exactly_and_fetch_reads_back(act, heads, d):
     pos = torch.arange(n, dtype=torch.int32, device=DEV) % 5
     before = rig.mem.clone()
     assert s3.s3_kv_append(rig.a, 1, n, rig.off_d, pos, x[0], x[1], rig.stream) == 0
-    got = rig.mem.view(2, 2, rig.N, rig.row).cpu().numpy()
-    old = before.view(2, 2, rig.N, rig.row).cpu().numpy()
+    got = rig.rows().cpu().numpy()
+    old = rig.rows(before).cpu().numpy()
     at = rig.offs + pos.cpu().numpy()
     for which in range(2):
         want = old[1, which].copy()
@@ -276,7 +283,7 @@ def test_step_checks_and_refused_entries():
     assert s3.s3_decode_step(rig.a, 0, n, off, pos, q, k, v, out, 2, 0.0, new, rig.stream) == 0
     torch.cuda.synchronize()
     assert (out[:3] == 0).all() and torch.isfinite(out[3]).all() and out[3].abs().sum() > 0
-    changed = (rig.mem != before).view(2, rig.N, rig.row).any(-1)
+    changed = (rig.rows() != rig.rows(before)).any(-1)[0]
     assert changed.nonzero()[:, 1].unique().tolist() == [int(rig.offs[3]) + 30]
     rig.close()
 

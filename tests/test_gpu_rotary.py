@@ -110,7 +110,7 @@ def test_norm_of_extremes():
 
 class Cache:
     def __init__(self, x, kv_dtype, preds, max_len=2048, granule=64):
-        self.x = x
+        self.x, self.kv_dtype = x, kv_dtype
         cfg = s3.make_config(2, x.heads, x.d, kv_dtype, granule, max_len, 0 if x.heads == x.kv else x.kv, x.act)
         bpt = s3.s3_kv_bytes_per_token(cfg)
         self.N = sum(s3.s3_kv_capacity_for(cfg, p) for p in preds)
@@ -120,6 +120,13 @@ class Cache:
         assert st == 0
         rc, self.ids, self.offs, _ = s3.s3_kv_alloc(self.a, preds)
         assert rc == len(preds)
+
+    def rows(self):
+        """The arena as stored rows [layers][2][N][row] (4-bit rows: codes and scales lie in planes of their own)."""
+        codes = self.x.kv * self.x.d // 2 if self.kv_dtype == s3.S3_MXFP4 else self.row
+        cut = 4 * self.N * codes
+        parts = [self.mem[:cut].view(2, 2, self.N, codes), self.mem[cut:].view(2, 2, self.N, self.row - codes)]
+        return torch.cat(parts, -1).cpu().numpy()
 
     def fetch(self, layer, off, pos):
         k, v = (torch.full((len(pos), self.x.kv, self.x.d), 7.0, dtype=TDT[self.x.act], device=DEV) for _ in range(2))
@@ -172,7 +179,7 @@ def test_append(case, kv_dtype, act):
     off, pos = off[mix], pos[mix]
     off_d, pos_d = torch.from_numpy(off.astype(np.int64)).to(DEV), torch.from_numpy(pos).to(DEV)
     live = (off >= 0) & (pos < 2048)
-    before = c.mem.view(2, 2, c.N, c.row).cpu().numpy()
+    before = c.rows()
     for rot in (x.rot_d, None):
         (q64, qm), (k64, km) = x.want(None if rot is not None else np.repeat(pos[None], axes, 0))
         q_out = torch.full((n, heads, d), 9.0, dtype=TDT[act], device=DEV)
@@ -180,7 +187,7 @@ def test_append(case, kv_dtype, act):
         torch.cuda.synchronize()
         close(q_out[torch.from_numpy(live)], q64[live], qm[live], act, case)
         assert (q_out[torch.from_numpy(~live)] == 9).all()
-        after = c.mem.view(2, 2, c.N, c.row).cpu().numpy()
+        after = c.rows()
         at = (off + pos)[live]
         k, v = c.fetch(1, off_d, pos_d)
         assert (k[torch.from_numpy(~live)] == 7).all()
@@ -189,7 +196,7 @@ def test_append(case, kv_dtype, act):
         other = Cache(x, kv_dtype, [f + r for f, r in runs])
         assert s3.s3_kv_append(other.a, 1, n, off_d, pos_d, x.k.contiguous(), x.v.contiguous()) == 0
         torch.cuda.synchronize()
-        plane = other.mem.view(2, 2, c.N, c.row).cpu().numpy()
+        plane = other.rows()
         assert np.array_equal(after[1, 1], plane[1, 1])
         untouched = np.ones(c.N, bool)
         untouched[at] = False
