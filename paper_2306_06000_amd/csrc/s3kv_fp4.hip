@@ -107,7 +107,7 @@ __device__ __forceinline__ void read_tile(Fp4Tile<128> &t, unsigned k, unsigned 
         : "v"(k), "v"(ks), "v"(v), "v"(vs)
         : "memory");
 }
-__device__ __forceinline__ void read_tile(Fp4Tile<256> &t, unsigned k, unsigned k2, unsigned ks, unsigned v, unsigned vs) {
+__device__ __forceinline__ void read_tile(Fp4Tile<256> &t, unsigned k, unsigned k2, unsigned ks, unsigned ks2, unsigned v, unsigned vs) {
     u32x2 w[8];
     asm volatile(
         "ds_read_b128 %0, %24\n\t"
@@ -115,9 +115,9 @@ __device__ __forceinline__ void read_tile(Fp4Tile<256> &t, unsigned k, unsigned 
         "ds_read_b128 %2, %24 offset:2048\n\t"
         "ds_read_b128 %3, %25 offset:2048\n\t"
         "ds_read_u8 %4, %26\n\t"
-        "ds_read_u8 %5, %26 offset:4\n\t"
+        "ds_read_u8 %5, %29\n\t"
         "ds_read_u8 %6, %26 offset:128\n\t"
-        "ds_read_u8 %7, %26 offset:132\n\t"
+        "ds_read_u8 %7, %29 offset:128\n\t"
         "ds_read_b64 %8, %27\n\t"
         "ds_read_b64 %9, %27 offset:512\n\t"
         "ds_read_b64 %10, %27 offset:1024\n\t"
@@ -138,7 +138,7 @@ __device__ __forceinline__ void read_tile(Fp4Tile<256> &t, unsigned k, unsigned 
         : "=&v"(t.k[0][0]), "=&v"(t.k[0][1]), "=&v"(t.k[1][0]), "=&v"(t.k[1][1]), "=&v"(t.ks[0][0]), "=&v"(t.ks[0][1]), "=&v"(t.ks[1][0]),
           "=&v"(t.ks[1][1]), "=&v"(w[0]), "=&v"(w[1]), "=&v"(w[2]), "=&v"(w[3]), "=&v"(w[4]), "=&v"(w[5]), "=&v"(w[6]), "=&v"(w[7]),
           "=&v"(t.vs[0]), "=&v"(t.vs[1]), "=&v"(t.vs[2]), "=&v"(t.vs[3]), "=&v"(t.vs[4]), "=&v"(t.vs[5]), "=&v"(t.vs[6]), "=&v"(t.vs[7])
-        : "v"(k), "v"(k2), "v"(ks), "v"(v), "v"(vs)
+        : "v"(k), "v"(k2), "v"(ks), "v"(v), "v"(vs), "v"(ks2)
         : "memory");
 #pragma unroll
     for (int e = 0; e < 8; e++) {
@@ -187,10 +187,11 @@ __device__ __forceinline__ void widen_pairs(const unsigned (&v)[8], const float 
     hi = pack_words(h[0], h[1], h[2], h[3]);
 }
 
-// What one wave does with the rows of a unit.  NH: heads of a unit (2 only for D = 64); NP: bf16 parts of a weight.
+// What one wave does with the rows of a unit: NH neighbouring heads, 128 or 256 elements.  NP: bf16 parts of a weight.
 template <int ACT, int D, int NH, int NP>
 struct Fp4Wave {
-    static constexpr int W = D == 256 ? 256 : 128, T = W / 128;
+    static constexpr int W = D * NH < 128 ? 128 : D * NH, T = W / 128;
+    static_assert(W == 128 || W == 256, "a unit");
     static constexpr int QP = ACT == S3_F16 ? 2 : 1;  // bf16 parts of a query
     static constexpr int QB = 16 / NH;                // columns of a head
     typedef Fp4Ring<W> Ring;
@@ -201,10 +202,9 @@ struct Fp4Wave {
     int lane, r, g;
     int code_bytes, scale_bytes;  // of a row
     int kh0, qb, per_head;  // first cached head, block of query heads, query heads of a cached head in it
-    bool second;            // the unit has two heads
-    int ksub, vsub, qsub, kblk, vel, khead, vhead, qhead;
-    int ko, kso, vo, vso;
-    bool column, q_here;
+    int heads;              // of the unit that there are
+    int qsub, qhead;        // this lane's column: its head of the unit, its query head
+    bool column;            // the column is one
     float m, l;
     f32x4 acc[8 * T];
 
@@ -216,27 +216,23 @@ struct Fp4Wave {
         scale_bytes = fp4_scale_bytes(a.H, D);
     }
 
-    // Which heads: of the A operand's lanes (K: block group g; V: elements of lane m = r), of the B operand's columns.
+    // The element of the unit (of its first head, where the element's head is not there) that a lane's data begin with: K, block g of half
+    // h; V, elements 8Tr ...
+    __device__ __forceinline__ int there(int element) const { return NH == 1 ? element % D : element < heads * D ? element : element % D; }
+    __device__ __forceinline__ int k_element(int h) const { return there(h * 128 + g * 32); }
+    __device__ __forceinline__ int v_element() const { return there(8 * T * r); }
+    __device__ __forceinline__ int k_head(int h) const { return NH == 1 ? 0 : (h * 128 + g * 32) / D; }
+
     __device__ __forceinline__ void set_column(int col) {
         const int unit = a.nqb == 1 ? col : col / a.nqb;
         qb = col - unit * a.nqb;
         kh0 = unit * NH;
-        second = NH == 2 && kh0 + 1 < a.H;
+        heads = min(NH, a.H - kh0);
         per_head = min(a.group - qb * QB, QB);
-        ksub = NH == 2 ? g >> 1 : 0;
-        vsub = qsub = NH == 2 ? r >> 3 : 0;
-        khead = kh0 + (second ? ksub : 0);
-        vhead = kh0 + (second ? vsub : 0);
-        kblk = D == 64 ? g & 1 : g;                             // (+ 4 for the second half of 256)
-        vel = D == 256 ? 16 * r : D == 64 ? 8 * (r & 7) : 8 * r;  // first element of the V words
-        ko = khead * (D / 2) + kblk * 16;
-        kso = khead * (D / 32) + kblk;
-        vo = vhead * (D / 2) + vel / 2;
-        vso = vhead * (D / 32) + vel / 32;
-        const int qi = (r % QB) + qb * QB;
+        qsub = NH == 1 ? 0 : r / QB;
+        const int qi = r % QB + qb * QB;
         qhead = (kh0 + qsub) * a.group + qi;
-        column = qi < a.group && (NH == 1 || qsub == 0 || second);
-        q_here = column && (D != 64 || (NH == 2 ? ksub == qsub : g < 2));
+        column = qi < a.group && qsub < heads;
     }
 
     // Issues the loads of a tile that begins at row `row` of the arena and of which `rows` rows (1 and more) are there; rows past them
@@ -246,22 +242,27 @@ struct Fp4Wave {
         const char *ks = a.kscale + row * scale_bytes, *vs = a.vscale + row * scale_bytes;
         const int last = min(rows, 32) - 1;
         constexpr int LPR = 64 / Ring::PER_LOAD;  // lanes a row
+        // Pieces of 128 bytes carry the streaming hint; of 64, the other half of a cache line is another wave's, which finds it in L2 if
+        // the line was not given up at once (512 contexts of 512..4096 rows, 32q/8kv x 128: 337 us with the hint, 284 without; of 128:
+        // 57 and 61).
+        constexpr int HINT = W == 256 ? 2 : 0;
         const int base = kh0 * (D / 2), piece = lane % LPR;
-        // (heads that are not there: pieces of the one that is)
-        const int keep = D != 64 || second ? LPR - 1 : 1;
+        // (heads that are not there, and what a head of 64 alone leaves of a unit: pieces of the first)
+        const int pieces = heads * (D / 32);
+        const auto piece_at = [&](int p) { return p < pieces ? p : p & (D / 32 - 1); };
 #pragma unroll
         for (int i = 0; i < Ring::LOADS; i++) {
             const int place = i * Ring::PER_LOAD + lane / LPR;
             const int swap = W == 256 ? (place >> 1) & 7 : (place >> 2) & 3;
-            const unsigned at = min(place, last) * code_bytes + base + ((piece ^ swap) & keep) * 16;
-            __builtin_amdgcn_global_load_lds((glb_void *)(kp + at), (lds_void *)(stage + i * 1024), 16, 0, 2);
+            const unsigned at = min(place, last) * code_bytes + base + piece_at(piece ^ swap) * 16;
+            __builtin_amdgcn_global_load_lds((glb_void *)(kp + at), (lds_void *)(stage + i * 1024), 16, 0, HINT);
         }
 #pragma unroll
         for (int i = 0; i < Ring::LOADS; i++) {
             const int place = i * Ring::PER_LOAD + lane / LPR;
             const int mine = (place & 16) + 4 * (place & 3) + ((place >> 2) & 3);
-            const unsigned at = min(mine, last) * code_bytes + base + (piece & keep) * 16;
-            __builtin_amdgcn_global_load_lds((glb_void *)(vp + at), (lds_void *)(stage + 32 * Ring::ROW + i * 1024), 16, 0, 2);
+            const unsigned at = min(mine, last) * code_bytes + base + piece_at(piece) * 16;
+            __builtin_amdgcn_global_load_lds((glb_void *)(vp + at), (lds_void *)(stage + 32 * Ring::ROW + i * 1024), 16, 0, HINT);
         }
         const int scales = kh0 * (D / 32) & ~3;
         char *s = stage + 64 * Ring::ROW;
@@ -276,13 +277,14 @@ struct Fp4Wave {
     }
     __device__ __forceinline__ void read(Fp4Tile<W> &t, const char *stage) const {
         const unsigned base = (unsigned)(uintptr_t)(lds_void *)stage, s = base + 64 * Ring::ROW;
-        const int shift = D == 64 && NH == 1 ? 2 * (kh0 & 1) : 0;  // (a unit's scales within their word)
-        const unsigned ks = s + r * 4 * T + shift + (D == 64 && (NH == 1 || !second) ? g & 1 : g);
+        const int shift = W > D * NH ? 2 * (kh0 & 1) : 0;  // (a head of 64 alone: its scales within their word)
+        // (of the second half of 256 elements: 4 bytes on; where its heads are not there, the first half's are read again)
+        const unsigned ks = s + r * 4 * T + shift + k_element(0) / 32;
         const unsigned v = base + 32 * Ring::ROW + g * Ring::ROW + r * 4 * T;
-        const unsigned vs = s + 128 * T + g * 16 * T + (W == 256 ? r >> 1 : shift + (D == 64 && (NH == 1 || !second) ? (r >> 2) & 1 : r >> 2));
+        const unsigned vs = s + 128 * T + g * 16 * T + shift + v_element() / 32;
         if constexpr (W == 256) {
             const unsigned k = base + r * 128 + ((g ^ ((r >> 1) & 7)) * 16), k2 = base + r * 128 + (((4 + g) ^ ((r >> 1) & 7)) * 16);
-            read_tile(t, k, k2, ks, v, vs);
+            read_tile(t, k, k2, ks, s + r * 8 + k_element(1) / 32, v, vs);
         } else {
             read_tile(t, base + r * 64 + ((g ^ (r >> 2)) * 16), ks, v, vs);
         }
@@ -296,7 +298,9 @@ struct Fp4Wave {
 #pragma unroll
             for (int i = 0; i < 4; i++) {
                 w[h][i] = (u32x4){0u, 0u, 0u, 0u};
-                if (q_here) w[h][i] = *(const u32x4 *)(a.q + (((int64_t)b * a.Hq + qhead) * D + h * 128 + kblk * 32 + i * 8) * 2);
+                // (the queries of a column meet their own head's elements, zeros meet the others')
+                if (column && (W > D * NH ? g < 2 : k_head(h) == qsub))
+                    w[h][i] = *(const u32x4 *)(a.q + (((int64_t)b * a.Hq + qhead) * D + (h * 128 + g * 32) % D + i * 8) * 2);
             }
 #pragma unroll
         for (int h = 0; h < T; h++)
@@ -338,23 +342,27 @@ struct Fp4Wave {
                 }
             }
         }
-        if (NH == 2 && __builtin_amdgcn_ballot_w64(t.ks[0][0] == 255u || t.ks[1][0] == 255u)) {
-            // a block that reads as NaN must not reach the other head's columns (NaN times their zeros)
+        bool nan = false;
 #pragma unroll
-            for (int u = 0; u < 2; u++) {
-                f32x4 c[2];
+        for (int h = 0; h < T; h++) nan = nan || t.ks[0][h] == 255u || t.ks[1][h] == 255u;
+        if (NH > 1 && __builtin_amdgcn_ballot_w64(nan)) {
+            // a block that reads as NaN must not reach the other heads' columns (NaN times their zeros)
 #pragma unroll
-                for (int sub = 0; sub < 2; sub++) {
-                    c[sub] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            for (int u = 0; u < 2; u++)
+#pragma unroll 1
+                for (int sub = 0; sub < heads; sub++) {
+                    f32x4 c = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        const bf16x8 k8 = widen_word(ksub == sub ? t.k[u][0][i] : 0u, ksub == sub ? fp4_scale(t.ks[u][0]) : 1.f);
+                    for (int h = 0; h < T; h++)
 #pragma unroll
-                        for (int part = 0; part < QP; part++) c[sub] = mfma_bf16(k8, q[part][0][i], c[sub]);
-                    }
+                        for (int i = 0; i < 4; i++) {
+                            const bool its = k_head(h) == sub;
+                            const bf16x8 k8 = widen_word(its ? t.k[u][h][i] : 0u, its ? fp4_scale(t.ks[u][h]) : 1.f);
+#pragma unroll
+                            for (int part = 0; part < QP; part++) c = mfma_bf16(k8, q[part][h][i], c);
+                        }
+                    if (qsub == sub) s[u] = c;
                 }
-                s[u] = qsub ? c[1] : c[0];
-            }
         }
         float p[8];
 #pragma unroll
@@ -417,17 +425,15 @@ struct Fp4Wave {
     // written to the arena (row `row`) by those that own the bytes.
     __device__ __forceinline__ void take_new_row(Fp4Tile<W> &t, int b, int64_t row, int rows) const {
         const int64_t at = row * code_bytes, scale_at = row * scale_bytes;
-        const bool k_own = r == 0 && (D != 64 || (NH == 2 ? ksub == 0 || second : g < 2));
-        const bool v_own = g == 0 && (D != 64 || (NH == 2 ? vsub == 0 || second : r < 8));
-        const char *ksrc = a.k_new + (((int64_t)b * a.H + khead) * D + kblk * 32) * 2;
-        const char *vsrc = a.v_new + (((int64_t)b * a.H + vhead) * D + vel) * 2;
+        const int present = heads * D, kbase = kh0 * D;  // elements of the unit that there are, of the row in front of it
+        const char *k_new = a.k_new + ((int64_t)b * a.H * D + kbase) * 2, *v_new = a.v_new + ((int64_t)b * a.H * D + kbase) * 2;
 #pragma unroll
         for (int h = 0; h < T; h++) {
             float x[4][8];
             unsigned most = 0;
 #pragma unroll
             for (int i = 0; i < 4; i++) {
-                widen8<ACT>(*(const u32x4 *)(ksrc + h * 256 + i * 16), x[i]);
+                widen8<ACT>(*(const u32x4 *)(k_new + k_element(h) * 2 + i * 16), x[i]);
 #pragma unroll
                 for (int e = 0; e < 8; e++) most = fp4_magnitude(x[i][e], most);
             }
@@ -435,9 +441,9 @@ struct Fp4Wave {
             u32x4 c;
 #pragma unroll
             for (int i = 0; i < 4; i++) c[i] = fp4_codes8(x[i], byte);
-            if (k_own) {
-                *(u32x4 *)(a.kplane + at + ko + 64 * h) = c;
-                a.kscale[scale_at + kso + 4 * h] = (char)byte;
+            if (r == 0 && h * 128 + g * 32 < present) {
+                *(u32x4 *)(a.kplane + at + (kbase + k_element(h)) / 2) = c;
+                a.kscale[scale_at + (kbase + k_element(h)) / 32] = (char)byte;
             }
 #pragma unroll
             for (int u = 0; u < 2; u++)
@@ -446,11 +452,12 @@ struct Fp4Wave {
                     t.ks[u][h] = byte;
                 }
         }
+        const bool v_own = g == 0 && 8 * T * r < present;
         float x[T][8];
         unsigned most = 0;
 #pragma unroll
         for (int h = 0; h < T; h++) {
-            widen8<ACT>(*(const u32x4 *)(vsrc + h * 16), x[h]);
+            widen8<ACT>(*(const u32x4 *)(v_new + v_element() * 2 + h * 16), x[h]);
 #pragma unroll
             for (int e = 0; e < 8; e++) most = fp4_magnitude(x[h][e], most);
         }
@@ -459,12 +466,12 @@ struct Fp4Wave {
 #pragma unroll
         for (int h = 0; h < T; h++) {
             const unsigned c = fp4_codes8(x[h], byte);
-            if (v_own) *(unsigned *)(a.vplane + at + vo + 4 * h) = c;
+            if (v_own) *(unsigned *)(a.vplane + at + (kbase + v_element()) / 2 + 4 * h) = c;
 #pragma unroll
             for (int e = 0; e < 8; e++)
                 if (16 * (e >> 2) + 4 * g + (e & 3) >= rows - 1) t.v[e][h] = c;
         }
-        if (v_own && vel % 32 == 0) a.vscale[scale_at + vso] = (char)byte;
+        if (v_own && v_element() % 32 == 0) a.vscale[scale_at + (kbase + v_element()) / 32] = (char)byte;
         const int used = a.H * (D / 32);
         if (kh0 + NH >= a.H && lane < scale_bytes - used) {  // zeros up to a multiple of 16 bytes
             a.kscale[scale_at + used + lane] = 0;
@@ -489,12 +496,12 @@ struct Fp4Wave {
 
 // The new lengths, and a zero output row for empty or refused contexts, by the workgroups in turn.
 template <int D>
-__device__ __forceinline__ void publish_lengths(const AttnArgs &a, const BatchView &bv) {
+__device__ __forceinline__ void publish_lengths(const AttnArgs &a) {
     for (int b = blockIdx.x; b < a.n; b += gridDim.x) {
         if (a.len_out && threadIdx.x == 0) a.len_out[b] = a.cur_len[b] + 1;
-        if (bv.len[b] == 0) {
+        if (checked_len(a, b) == 0) {
             const float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            for (int e = threadIdx.x; e < a.Hq * D / 8; e += 256) store_out8(a.out, a.out_dtype, ((int64_t)b * a.Hq * D / 8 + e) * 8, z);
+            for (int e = threadIdx.x; e < a.Hq * D / 8; e += blockDim.x) store_out8(a.out, a.out_dtype, ((int64_t)b * a.Hq * D / 8 + e) * 8, z);
         }
     }
 }
@@ -516,7 +523,7 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_team_kernel(const AttnArgs a)
     // a wave's ring takes its sums of the columns in use when its rows are done: STRIDE floats a column
     constexpr int RING = 2 * Wave::Ring::STAGE;
     static_assert(16 * STRIDE * 4 <= RING, "a wave's sums fit its ring");
-    publish_lengths<D>(a, bv);
+    publish_lengths<D>(a);
     Wave w(a, rings + ts * RING);
     // Work in the order of eighths: workgroup b (XCD b % 8) takes the chunks whose number leaves the same remainder, so that the
     // columns of a chunk, whose bytes share cache lines, are on one XCD's L2.
@@ -552,7 +559,7 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_team_kernel(const AttnArgs a)
         }
 
         // the four waves meet: columns in use, compact (head, query)
-        const int slot = w.qsub * w.per_head + (w.r % QB), n_cols = (w.second ? 2 : 1) * w.per_head;
+        const int slot = w.qsub * w.per_head + (w.r % QB), n_cols = w.heads * w.per_head;
         const float l = sum_over_rows(w.l);
         if (w.column && w.g == 0) {
             comb_m[ts][slot] = w.m;
@@ -569,7 +576,7 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_team_kernel(const AttnArgs a)
         // a thread: eight elements of one column
         const int slices = n_cols * (D / 8);
         for (int i = threadIdx.x; i < slices; i += 256) {
-            const int c = i / (D / 8), dl = i % (D / 8), sub = NH == 2 && c >= w.per_head ? 1 : 0;
+            const int c = i / (D / 8), dl = i % (D / 8), sub = NH == 1 ? 0 : c / w.per_head;
             const int h = (w.kh0 + sub) * a.group + w.qb * QB + (c - sub * w.per_head);
             float mm = -INFINITY, ll = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -579,7 +586,7 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_team_kernel(const AttnArgs a)
             for (int x = 0; x < TS; x++) {
                 const float wt = fast_exp2(comb_m[x][c] - ref);
                 ll += wt * comb_l[x][c];
-                const float *src = (const float *)(rings + x * RING) + c * STRIDE + sub * 64 + dl * 8;
+                const float *src = (const float *)(rings + x * RING) + c * STRIDE + sub * D + dl * 8;
                 const f32x4 x0 = *(const f32x4 *)src, x1 = *(const f32x4 *)(src + 4);
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
@@ -612,13 +619,51 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_team_kernel(const AttnArgs a)
             if (last_of_context) {
                 if (a.merge_sync) __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
                 for (int i = threadIdx.x; i < slices; i += 256) {
-                    const int c = i / (D / 8), dl = i % (D / 8), sub = NH == 2 && c >= w.per_head ? 1 : 0;
+                    const int c = i / (D / 8), dl = i % (D / 8), sub = NH == 1 ? 0 : c / w.per_head;
                     merge_chunks<D, true>(a, it.slot0, a.Hq, it.b, (w.kh0 + sub) * a.group + w.qb * QB + (c - sub * w.per_head), dl, it.nchunks);
                 }
             }
         }
         __syncthreads();  // LDS is used again by the next item
     }
+}
+
+// Exclusive prefix sums of the contexts' tiles into pre[0..n], by the whole workgroup; returns the total (longest: the rows of the
+// longest context).
+__device__ __forceinline__ int tile_prefix(const AttnArgs &a, int *pre, int *wave_sums, int &longest) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, nwaves = blockDim.x >> 6;
+    constexpr int E = 4;
+    int total = 0;
+    for (int base = 0; base < a.n; base += E * (int)blockDim.x) {
+        int64_t off[E];
+        int len[E], sum = 0, mx = 0;
+        load_entries<E>(a, base + tid * E, off, len);
+#pragma unroll
+        for (int e = 0; e < E; e++) {
+            sum += (len[e] + 31) >> 5;
+            mx = max(mx, len[e]);
+        }
+        const int incl = wave_inclusive_scan(sum);
+        mx = wave_max_nonneg(mx);
+        if (lane == 63) {
+            wave_sums[wave] = incl;
+            wave_sums[S3_MAX_WAVES + wave] = mx;
+        }
+        __syncthreads();
+        const int upto = wave_inclusive_scan(lane < nwaves ? wave_sums[lane] : 0);
+        longest = max(longest, wave_max_nonneg(lane < nwaves ? wave_sums[S3_MAX_WAVES + lane] : 0));
+        int run = total + incl - sum + (wave > 0 ? __builtin_amdgcn_readlane(upto, wave - 1) : 0);
+        total += __builtin_amdgcn_readlane(upto, nwaves - 1);
+#pragma unroll
+        for (int e = 0; e < E; e++) {
+            const int b = base + tid * E + e;
+            if (b < a.n) pre[b] = run;
+            run += (len[e] + 31) >> 5;
+        }
+        if (tid == 0) pre[a.n] = total;
+        __syncthreads();
+    }
+    return total;
 }
 
 // Many (context, column) pairs: the tiles of all contexts laid end to end are cut into equal shares, one a wave and column, so that
@@ -628,31 +673,31 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_team_kernel(const AttnArgs a)
 // Contexts of few tiles are not cut: a share takes those that begin in it.
 #define S3_FP4_UNCUT 8
 template <int ACT, int D, int NH, int NP>
-__global__ void __launch_bounds__(256, 2) attn_fp4_share_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(512, 2) attn_fp4_share_kernel(const AttnArgs a) {
     typedef Fp4Wave<ACT, D, NH, NP> Wave;
     constexpr int W = Wave::W, T = Wave::T, QB = Wave::QB;
-    extern __shared__ __align__(16) char dyn_lds[];  // the batch view in tiles, the waves' rings
-    __shared__ int wave_sums[3 * S3_MAX_WAVES];
+    extern __shared__ __align__(16) char dyn_lds[];  // tiles in front of every context, [n + 1]; the waves' rings
+    __shared__ int wave_sums[2 * S3_MAX_WAVES];
+    int *pre = (int *)dyn_lds;
+    char *rings = dyn_lds + (((a.n + 1) * 4 + 15) & ~15);
     int longest = 0;
-    const BatchView bv = build_tile_view<32>(a, dyn_lds, wave_sums, longest);
-    char *rings = dyn_lds + ((batch_view_bytes(a.n, 1) + 15) & ~(size_t)15);
-    publish_lengths<D>(a, bv);
+    const int total = tile_prefix(a, pre, wave_sums, longest);
+    publish_lengths<D>(a);
     const int ts = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // Neighbouring columns, whose bytes share cache lines, are on neighbouring waves, and those on one XCD (workgroup b is on XCD b % 8).
     const int rank = (gridDim.x & 7) == 0 ? (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3) : blockIdx.x;
-    const int place = rank * 4 + ts;
+    const int place = rank * 8 + ts;
     const int share = place / a.columns, col = place - share * a.columns;
-    const int total = __builtin_amdgcn_readfirstlane(bv.total);
-    const bool cut = __builtin_amdgcn_readfirstlane(longest) > 32 * S3_FP4_UNCUT;
+    const bool cut = longest > 32 * S3_FP4_UNCUT;
     const int size = max((total + a.wave_shares - 1) / a.wave_shares, 1);
     if (share >= a.wave_shares || share * (int64_t)size >= total) return;
     int t0 = share * size, t1 = min(total, t0 + size);
-    int b = __builtin_amdgcn_readfirstlane(find_sequence(bv.pre, a.n, t0));  // the context that holds tile t0
+    int b = __builtin_amdgcn_readfirstlane(find_sequence(pre, a.n, t0));  // the context that holds tile t0
     if (!cut) {  // from the first context that begins at t0 or behind it to the last that begins in front of t1
-        if (__builtin_amdgcn_readfirstlane(bv.pre[b]) < t0) b++;
-        t0 = __builtin_amdgcn_readfirstlane(bv.pre[b]);
+        if (__builtin_amdgcn_readfirstlane(pre[b]) < t0) b++;
+        t0 = __builtin_amdgcn_readfirstlane(pre[b]);
         if (t0 >= t1) return;
-        t1 = __builtin_amdgcn_readfirstlane(bv.pre[find_sequence(bv.pre, a.n, t1 - 1) + 1]);
+        t1 = __builtin_amdgcn_readfirstlane(pre[find_sequence(pre, a.n, t1 - 1) + 1]);
     }
     constexpr int DEEP = Wave::Ring::DEEP;
     Wave w(a, rings + ts * DEEP * Wave::Ring::STAGE);
@@ -667,20 +712,20 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_share_kernel(const AttnArgs a
     };
     const auto open = [&](Cursor &c, int tile) {  // the context that holds `tile`, from context c.b on
         while (true) {
-            c.end = __builtin_amdgcn_readfirstlane(bv.pre[c.b + 1]);
+            c.end = __builtin_amdgcn_readfirstlane(pre[c.b + 1]);
             if (tile < c.end) break;
             c.b++;
         }
-        c.begin = __builtin_amdgcn_readfirstlane(bv.pre[c.b]);
-        c.len = __builtin_amdgcn_readfirstlane(bv.len[c.b]);
-        c.off = uniform64(bv.off[c.b]);
+        c.begin = __builtin_amdgcn_readfirstlane(pre[c.b]);
+        c.off = uniform64(a.slot_off[c.b]);
+        c.len = __builtin_amdgcn_readfirstlane(a.cur_len[c.b]) + a.len_add;  // (a context with tiles: it has been checked)
         c.tile = tile;
     };
     const auto finish = [&](const Cursor &c) {  // the share's part of context c.b is folded in
         const int first = max(c.begin, t0), last = min(c.end, t1);
         const float l = sum_over_rows(w.l);
-        const bool mine = w.column && (D != 64 || (NH == 2 ? (w.g >> 1) == w.qsub : w.g < 2));
-        const int e0 = 8 * T * 4 * w.g - (NH == 2 ? 64 * w.qsub : 0);  // this lane's first element of its head
+        const int e0 = 32 * T * w.g - D * w.qsub;  // this lane's first element, of its column's head
+        const bool mine = w.column && e0 >= 0 && e0 < D;
         if (first == c.begin && last == c.end) {
             const float inv = 1.f / l;
             if (mine) {
@@ -755,9 +800,9 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_share_kernel(const AttnArgs a
     for (int k = 0; k < 2; k++) {
         if (!(who >> k & 1)) continue;
         const Pending p = {k ? tail.b : head.b, k ? tail.first : head.first, k ? tail.count : head.count};
-        const int slices = (w.second ? 2 : 1) * w.per_head * (D / 8);
+        const int slices = w.heads * w.per_head * (D / 8);
         for (int i = w.lane; i < slices; i += 64) {
-            const int c = i / (D / 8), dl = i % (D / 8), sub = NH == 2 && c >= w.per_head ? 1 : 0;
+            const int c = i / (D / 8), dl = i % (D / 8), sub = NH == 1 ? 0 : c / w.per_head;
             merge_chunks<D, true>(a, p.first + p.b, a.Hq, p.b, (w.kh0 + sub) * a.group + w.qb * QB + (c - sub * w.per_head), dl, p.count);
         }
     }
@@ -766,7 +811,8 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_share_kernel(const AttnArgs a
 template <int ACT, int NP, bool SHARES>
 static attn_fn pick_fp4(int d, int nh) {
     if (SHARES) {
-        if (d == 64) return nh == 2 ? attn_fp4_share_kernel<ACT, 64, 2, NP> : attn_fp4_share_kernel<ACT, 64, 1, NP>;
+        if (d == 64) return nh == 4 ? attn_fp4_share_kernel<ACT, 64, 4, NP> : nh == 2 ? attn_fp4_share_kernel<ACT, 64, 2, NP> : attn_fp4_share_kernel<ACT, 64, 1, NP>;
+        if (d == 128 && nh == 2) return attn_fp4_share_kernel<ACT, 128, 2, NP>;
         return d == 128 ? attn_fp4_share_kernel<ACT, 128, 1, NP> : d == 256 ? attn_fp4_share_kernel<ACT, 256, 1, NP> : nullptr;
     }
     if (d == 64) return nh == 2 ? attn_fp4_team_kernel<ACT, 64, 2, NP> : attn_fp4_team_kernel<ACT, 64, 1, NP>;
@@ -774,8 +820,9 @@ static attn_fn pick_fp4(int d, int nh) {
 }
 
 attn_fn s3i_pick_fp4(int act, int d, int heads_per_unit, bool wide_out, bool shares, int *lds) {
-    const int stage = d == 256 ? Fp4Ring<256>::STAGE : Fp4Ring<128>::STAGE;
-    *lds = 4 * stage * (shares ? d == 256 ? Fp4Ring<256>::DEEP : Fp4Ring<128>::DEEP : 2);
+    const bool wide = d * heads_per_unit == 256;
+    const int stage = wide ? Fp4Ring<256>::STAGE : Fp4Ring<128>::STAGE;
+    *lds = shares ? 8 * stage * (wide ? Fp4Ring<256>::DEEP : Fp4Ring<128>::DEEP) : 4 * stage * 2;
     if (act == S3_F16) {
         if (wide_out) return shares ? pick_fp4<S3_F16, 3, true>(d, heads_per_unit) : pick_fp4<S3_F16, 3, false>(d, heads_per_unit);
         return shares ? pick_fp4<S3_F16, 2, true>(d, heads_per_unit) : pick_fp4<S3_F16, 2, false>(d, heads_per_unit);

@@ -836,11 +836,12 @@ static size_t chunk_slots(const s3_arena *a, int n, int n_hg, size_t slot_bytes,
     return (size_t)(want > 0 && want + n > whole ? want + n : whole);
 }
 
-// Rows of 4-bit blocks: how a launch over n contexts is laid out.  A unit is what a wave's 16-byte loads cover of a row: a head
-// of 128 or 256, two neighbouring heads of 64 while their query heads fit the sixteen columns together.  A column (of the work
-// list) is a unit and up to sixteen (eight a head) of its query heads.
+// Rows of 4-bit blocks: how a launch over n contexts is laid out.  A unit is what a wave takes of a row, 128 or 256 elements of one head
+// or of neighbouring ones; a column (of the work list) is a unit and up to sixteen of its query heads.
+#define S3_FP4_SHARES 2
 struct Fp4Plan {
     int heads_per_unit, blocks_per_head, columns;
+    int counted;    // columns that the arrival counters have room for: the most of any n
     bool shares;    // equal shares of all rows, one a wave (attn_fp4_share_kernel), or chunks of contexts, one a workgroup
     int32_t few;    // chunks that few contexts are cut into, 0: chunks of `chunk` rows
     int chunk;
@@ -850,20 +851,28 @@ static Fp4Plan fp4_plan(const s3_arena *a, int n) {
     Fp4Plan p;
     const int D = a->cfg.head_dim, Hkv = a->cfg.n_kv_heads, group = a->cfg.n_heads / Hkv;
     const int64_t cus = a->num_cus > 0 ? a->num_cus : 256;
-    p.heads_per_unit = D == 64 && Hkv > 1 && group <= 8 ? 2 : 1;
-    const int width = 16 / p.heads_per_unit;
-    p.blocks_per_head = (group + width - 1) / width;
-    p.columns = (Hkv + p.heads_per_unit - 1) / p.heads_per_unit * p.blocks_per_head;
+    // neighbouring heads share a unit while their query heads fit the sixteen columns together
+    const auto lay_out = [&](int widest) {
+        p.heads_per_unit = 1;
+        while (2 * p.heads_per_unit * D <= widest && p.heads_per_unit < Hkv && 2 * p.heads_per_unit * group <= 16) p.heads_per_unit *= 2;
+        const int width = 16 / p.heads_per_unit;
+        p.blocks_per_head = (group + width - 1) / width;
+        p.columns = (Hkv + p.heads_per_unit - 1) / p.heads_per_unit * p.blocks_per_head;
+    };
+    lay_out(128);
+    p.counted = p.columns;
+    lay_out(256);  // (never more columns)
     p.chunk = a->chunk > 0 ? a->chunk : 1024;
     const size_t slot_bytes = (size_t)a->cfg.n_heads * ((size_t)D * sizeof(float) + sizeof(float2));
-    const int64_t fixed = (int64_t)((S3_STATIC_SCRATCH_BYTES - counters_bytes(p.columns)) / slot_bytes);
     const int64_t most = 8 * cus / p.columns;  // shares of a column: a wave each, eight waves a compute unit
-    p.shares = a->chunk <= 0 && a->grid_blocks <= 0 && p.columns <= 4 * cus && n * (int64_t)p.columns >= 4 * cus;
+    p.shares = a->chunk <= 0 && a->grid_blocks <= 0 && p.columns <= 8 * cus && n * (int64_t)p.columns >= S3_FP4_SHARES * cus;
     p.few = 0;
     if (p.shares) {
         p.slots = (size_t)(most + n);
         return p;
     }
+    lay_out(128);
+    const int64_t fixed = (int64_t)((S3_STATIC_SCRATCH_BYTES - counters_bytes(p.counted)) / slot_bytes);
     const int64_t whole = (int64_t)n * ((a->cfg.max_len + p.chunk - 1) / p.chunk);
     const int64_t fit = 2 * cus / p.columns;  // workgroups of a column that run at once
     int64_t want = a->chunk <= 0 && n < fit ? fit : 0;
@@ -894,7 +903,7 @@ static size_t scratch_need(const s3_arena *a, int n) {
         }
         if (slots > most) most = slots;
     }
-    const int columns = kind == 5 ? fp4_plan(a, 1).columns : kind == 0 || kind == 3 ? n_hg : (int)gqa_columns(a);
+    const int columns = kind == 5 ? fp4_plan(a, 1).counted : kind == 0 || kind == 3 ? n_hg : (int)gqa_columns(a);
     return counters_bytes(columns) + most * slot_bytes;
 }
 
@@ -1122,18 +1131,17 @@ static int launch_fp4(s3_arena *a, const AttnCall &c) {
     args.group = a->cfg.n_heads / a->cfg.n_kv_heads;
     args.nqb = p.blocks_per_head;
     args.columns = p.columns;
-    int rc = place_scratch(a, args, counters_bytes(p.columns), p.slots, c);
+    int rc = place_scratch(a, args, counters_bytes(p.counted), p.slots, c);
     if (rc != S3_OK) return rc;
     const int cus = a->num_cus > 0 ? a->num_cus : 256;
     if (p.shares) {
         args.ncls = 1;
-        const size_t dyn_lds = ((batch_view_lds(c.n, 1) + 15) & ~(size_t)15) + lds;
+        const size_t dyn_lds = (((size_t)(c.n + 1) * 4 + 15) & ~(size_t)15) + lds;
         int per_cu = 0;
-        rc = resident_per_cu((const void *)fn, 256, dyn_lds, &per_cu);
+        rc = resident_per_cu((const void *)fn, 512, dyn_lds, &per_cu);
         if (rc != S3_OK) return rc;
-        if (per_cu > 2) per_cu = 2;
-        args.wave_shares = 4 * cus * per_cu / p.columns;
-        return launch_attn_kernels(a, fn, cus * per_cu, 256, dyn_lds, c.stream, args, 0, !c.static_scratch);
+        args.wave_shares = 8 * cus / p.columns;
+        return launch_attn_kernels(a, fn, cus, 512, dyn_lds, c.stream, args, 0, !c.static_scratch);
     }
     while (args.ncls > 1 && batch_view_lds(c.n, args.ncls) + lds > (size_t)156 * 1024) args.ncls--;
     const size_t dyn_lds = ((batch_view_lds(c.n, args.ncls) + 15) & ~(size_t)15) + lds;
