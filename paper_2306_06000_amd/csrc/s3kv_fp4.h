@@ -12,6 +12,7 @@
 #include "s3kv_device.h"
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 __host__ __device__ __forceinline__ int fp4_code_bytes(int heads, int d) { return heads * (d / 2); }

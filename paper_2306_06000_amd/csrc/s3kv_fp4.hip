@@ -6,8 +6,8 @@
 // exact in bf16) with up to 16 query heads as columns, also for a single one: 17 bits hold four elements, so the vector ALU
 // would need more instructions for them than the memory leaves time for.
 //   S^T = K Q^T   A operand: lane (r, g) holds block g (32 elements, one scale) of row r as it lies in memory, a 16-byte load;
-//                 the four products of a unit of 128 take a word of it each, Q^T in the same element order.  An fp16 query is
-//                 the exact sum of two bf16 parts, two products.
+//                 the four products of a unit of 128 take a word of it each, Q^T in the same element order; beside fp16 queries
+//                 the codes are widened to fp16.
 //   O^T += V^T P^T  A operand: lane (m, g) holds elements 8m .. 8m+7 (256: 16m ..) of the eight rows 4g .. 4g+3 and 16+4g ..
 //                 16+4g+3 of the tile, one word a row: after widening, pairs of rows are brought together by byte permutes, and
 //                 output tile i gets the elements 8m + i.  No row passes through LDS.  The accumulator layout of S^T is the B
@@ -152,6 +152,10 @@ __device__ __forceinline__ f32x4 mfma_bf16(const bf16x8 a, const bf16x8 b, const
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
+__device__ __forceinline__ f32x4 mfma_f16(const f16x8 a, const f16x8 b, const f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
 __device__ __forceinline__ bf16x8 pack_words(const unsigned a, const unsigned b, const unsigned c, const unsigned d) {
     const u32x4 w = {a, b, c, d};
     return __builtin_bit_cast(bf16x8, w);
@@ -161,6 +165,14 @@ __device__ __forceinline__ bf16x8 pack_words(const unsigned a, const unsigned b,
 __device__ __forceinline__ bf16x8 widen_word(const unsigned w, const float scale) {
     return pack_words(__builtin_bit_cast(unsigned, fp4_widen2<0>(w, scale)), __builtin_bit_cast(unsigned, fp4_widen2<1>(w, scale)),
                       __builtin_bit_cast(unsigned, fp4_widen2<2>(w, scale)), __builtin_bit_cast(unsigned, fp4_widen2<3>(w, scale)));
+}
+
+__device__ __forceinline__ f16x8 widen_word_f16(const unsigned w, const float scale) {
+    const u32x4 x = {__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 0)),
+                     __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 1)),
+                     __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 2)),
+                     __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 3))};
+    return __builtin_bit_cast(f16x8, x);
 }
 
 // Two fp32 numbers as a word of two bf16 (nearest, ties to even); what that leaves of them stays in x0, x1.
@@ -192,13 +204,12 @@ template <int ACT, int D, int NH, int NP>
 struct Fp4Wave {
     static constexpr int W = D * NH < 128 ? 128 : D * NH, T = W / 128;
     static_assert(W == 128 || W == 256, "a unit");
-    static constexpr int QP = ACT == S3_F16 ? 2 : 1;  // bf16 parts of a query
     static constexpr int QB = 16 / NH;                // columns of a head
     typedef Fp4Ring<W> Ring;
 
     const AttnArgs &a;
     char *ring;  // this wave's tiles on their way
-    bf16x8 q[QP][T][4];
+    u32x4 q[T][4];  // the queries of this lane's column, of type ACT, as the B operand takes them
     int lane, r, g;
     int code_bytes, scale_bytes;  // of a row
     int kh0, qb, per_head;  // first cached head, block of query heads, query heads of a cached head in it
@@ -233,19 +244,17 @@ struct Fp4Wave {
         const int qi = r % QB + qb * QB;
         qhead = (kh0 + qsub) * a.group + qi;
         column = qi < a.group && qsub < heads;
+        whole = offsets(31);
     }
 
-    // Issues the loads of a tile that begins at row `row` of the arena and of which `rows` rows (1 and more) are there; rows past them
-    // repeat the last one, whose values they then carry into the products with a weight of 0.
-    __device__ __forceinline__ void issue(char *stage, int64_t row, int rows) const {
-        const char *kp = a.kplane + row * code_bytes, *vp = a.vplane + row * code_bytes;
-        const char *ks = a.kscale + row * scale_bytes, *vs = a.vscale + row * scale_bytes;
-        const int last = min(rows, 32) - 1;
+    // Where a lane's pieces of a tile are, in bytes from the tile's first row; rows past `last` repeat that one, whose values they then
+    // carry into the products with a weight of 0.
+    struct Offsets {
+        unsigned k[Ring::LOADS], v[Ring::LOADS], s[T];
+    };
+    __device__ __forceinline__ Offsets offsets(int last) const {
+        Offsets o;
         constexpr int LPR = 64 / Ring::PER_LOAD;  // lanes a row
-        // Pieces of 128 bytes carry the streaming hint; of 64, the other half of a cache line is another wave's, which finds it in L2 if
-        // the line was not given up at once (512 contexts of 512..4096 rows, 32q/8kv x 128: 337 us with the hint, 284 without; of 128:
-        // 57 and 61).
-        constexpr int HINT = W == 256 ? 2 : 0;
         const int base = kh0 * (D / 2), piece = lane % LPR;
         // (heads that are not there, and what a head of 64 alone leaves of a unit: pieces of the first)
         const int pieces = heads * (D / 32);
@@ -254,25 +263,41 @@ struct Fp4Wave {
         for (int i = 0; i < Ring::LOADS; i++) {
             const int place = i * Ring::PER_LOAD + lane / LPR;
             const int swap = W == 256 ? (place >> 1) & 7 : (place >> 2) & 3;
-            const unsigned at = min(place, last) * code_bytes + base + piece_at(piece ^ swap) * 16;
-            __builtin_amdgcn_global_load_lds((glb_void *)(kp + at), (lds_void *)(stage + i * 1024), 16, 0, HINT);
-        }
-#pragma unroll
-        for (int i = 0; i < Ring::LOADS; i++) {
-            const int place = i * Ring::PER_LOAD + lane / LPR;
-            const int mine = (place & 16) + 4 * (place & 3) + ((place >> 2) & 3);
-            const unsigned at = min(mine, last) * code_bytes + base + piece_at(piece) * 16;
-            __builtin_amdgcn_global_load_lds((glb_void *)(vp + at), (lds_void *)(stage + 32 * Ring::ROW + i * 1024), 16, 0, HINT);
+            const int its = (place & 16) + 4 * (place & 3) + ((place >> 2) & 3);
+            o.k[i] = min(place, last) * code_bytes + base + piece_at(piece ^ swap) * 16;
+            o.v[i] = min(its, last) * code_bytes + base + piece_at(piece) * 16;
         }
         const int scales = kh0 * (D / 32) & ~3;
+#pragma unroll
+        for (int i = 0; i < T; i++) o.s[i] = W == 256 ? min(lane >> 1, last) * scale_bytes + scales + (lane & 1) * 4 : min(lane & 31, last) * scale_bytes + scales;
+        return o;
+    }
+
+    Offsets whole;  // of a tile with all its rows
+
+    // Issues the loads of a tile that begins at row `row` of the arena and of which `rows` rows (1 and more) are there.
+    __device__ __forceinline__ void issue(char *stage, int64_t row, int rows) const {
+        if (rows >= 32) issue(stage, row, whole);
+        else issue(stage, row, offsets(rows - 1));
+    }
+    __device__ __forceinline__ void issue(char *stage, int64_t row, const Offsets &o) const {
+        const char *kp = a.kplane + row * code_bytes, *vp = a.vplane + row * code_bytes;
+        const char *ks = a.kscale + row * scale_bytes, *vs = a.vscale + row * scale_bytes;
+        // Pieces of 128 bytes carry the streaming hint; of 64, the other half of a cache line is another wave's, which finds it in L2 if
+        // the line was not given up at once (512 contexts of 512..4096 rows, 32q/8kv x 128: 337 us with the hint, 284 without; of 128:
+        // 57 and 61).
+        constexpr int HINT = W == 256 ? 2 : 0;
+#pragma unroll
+        for (int i = 0; i < Ring::LOADS; i++) __builtin_amdgcn_global_load_lds((glb_void *)(kp + o.k[i]), (lds_void *)(stage + i * 1024), 16, 0, HINT);
+#pragma unroll
+        for (int i = 0; i < Ring::LOADS; i++)
+            __builtin_amdgcn_global_load_lds((glb_void *)(vp + o.v[i]), (lds_void *)(stage + 32 * Ring::ROW + i * 1024), 16, 0, HINT);
         char *s = stage + 64 * Ring::ROW;
-        if (W == 256) {
-            const unsigned at = min(lane >> 1, last) * scale_bytes + scales + (lane & 1) * 4;
-            __builtin_amdgcn_global_load_lds((glb_void *)(ks + at), (lds_void *)s, 4, 0, 0);
-            __builtin_amdgcn_global_load_lds((glb_void *)(vs + at), (lds_void *)(s + 256), 4, 0, 0);
+        if constexpr (W == 256) {
+            __builtin_amdgcn_global_load_lds((glb_void *)(ks + o.s[0]), (lds_void *)s, 4, 0, 0);
+            __builtin_amdgcn_global_load_lds((glb_void *)(vs + o.s[1]), (lds_void *)(s + 256), 4, 0, 0);
         } else {
-            const unsigned at = min(lane & 31, last) * scale_bytes + scales;
-            __builtin_amdgcn_global_load_lds((glb_void *)((lane < 32 ? ks : vs) + at), (lds_void *)s, 4, 0, 0);
+            __builtin_amdgcn_global_load_lds((glb_void *)((lane < 32 ? ks : vs) + o.s[0]), (lds_void *)s, 4, 0, 0);
         }
     }
     __device__ __forceinline__ void read(Fp4Tile<W> &t, const char *stage) const {
@@ -290,40 +315,60 @@ struct Fp4Wave {
         }
     }
 
-    // Sequence b's queries (fp16: two exact bf16 parts each); nothing folded in yet.
+    // Sequence b's queries; nothing folded in yet.
     __device__ __forceinline__ void begin(int b) {
-        u32x4 w[T][4];
 #pragma unroll
         for (int h = 0; h < T; h++)
 #pragma unroll
             for (int i = 0; i < 4; i++) {
-                w[h][i] = (u32x4){0u, 0u, 0u, 0u};
+                q[h][i] = (u32x4){0u, 0u, 0u, 0u};
                 // (the queries of a column meet their own head's elements, zeros meet the others')
                 if (column && (W > D * NH ? g < 2 : k_head(h) == qsub))
-                    w[h][i] = *(const u32x4 *)(a.q + (((int64_t)b * a.Hq + qhead) * D + (h * 128 + g * 32) % D + i * 8) * 2);
-            }
-#pragma unroll
-        for (int h = 0; h < T; h++)
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                if (QP == 1) {
-                    q[0][h][i] = __builtin_bit_cast(bf16x8, w[h][i]);
-                } else {
-                    float x[8];
-                    widen8<ACT>(w[h][i], x);
-#pragma unroll
-                    for (int part = 0; part < QP; part++) {
-                        u32x4 p;
-#pragma unroll
-                        for (int e = 0; e < 4; e++) p[e] = take_bf16_part(x[2 * e], x[2 * e + 1]);
-                        q[part][h][i] = __builtin_bit_cast(bf16x8, p);
-                    }
-                }
+                    q[h][i] = *(const u32x4 *)(a.q + (((int64_t)b * a.Hq + qhead) * D + (h * 128 + g * 32) % D + i * 8) * 2);
             }
         m = -INFINITY;
         l = 0.f;
 #pragma unroll
         for (int i = 0; i < 8 * T; i++) acc[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+
+    // Blocks that the products of fold() do not take: with several heads, those that read as NaN, which must not reach the other heads'
+    // columns (NaN times their zeros); beside fp16 queries, those with a scale under which a code is no fp16 number (appended rows have
+    // none: their scales are 101 to 140, or 1 for a block of zeros, and a scale below 104 only where no code is odd).
+    __device__ __forceinline__ static bool special(unsigned byte) {
+        return ACT == S3_F16 ? byte - 101u > 39u && byte > 1u : NH > 1 && byte == 255u;
+    }
+    // The scores of a tile with such blocks: head by head, widened to bf16 (fp16 queries are the exact sum of two bf16 parts).
+    __device__ __forceinline__ void special_scores(const Fp4Tile<W> &t, f32x4 (&s)[2]) const {
+#pragma unroll
+        for (int u = 0; u < 2; u++)
+#pragma unroll 1
+            for (int sub = 0; sub < heads; sub++) {
+                f32x4 c = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int h = 0; h < T; h++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const bool its = NH == 1 || k_head(h) == sub;
+                        const bf16x8 k8 = widen_word(its ? t.k[u][h][i] : 0u, its ? fp4_scale(t.ks[u][h]) : 1.f);
+                        if (ACT == S3_BF16) {
+                            c = mfma_bf16(k8, __builtin_bit_cast(bf16x8, q[h][i]), c);
+                        } else {
+                            u32x4 w = q[h][i];
+                            asm volatile("" : "+v"(w));  // (taken apart here, and not kept in parts)
+                            float x[8];
+                            widen8<ACT>(w, x);
+#pragma unroll
+                            for (int part = 0; part < 2; part++) {
+                                u32x4 p;
+#pragma unroll
+                                for (int e = 0; e < 4; e++) p[e] = take_bf16_part(x[2 * e], x[2 * e + 1]);
+                                c = mfma_bf16(k8, __builtin_bit_cast(bf16x8, p), c);
+                            }
+                        }
+                    }
+                if (qsub == sub) s[u] = c;
+            }
     }
 
     // What a tile holds is folded into (m, l, acc); rows: those of the tile and behind it (fewer than 32: the last tile).
@@ -336,33 +381,16 @@ struct Fp4Wave {
             for (int i = 0; i < 4; i++) {
 #pragma unroll
                 for (int u = 0; u < 2; u++) {
-                    const bf16x8 k8 = widen_word(t.k[u][h][i], scale[u]);
-#pragma unroll
-                    for (int part = 0; part < QP; part++) s[u] = mfma_bf16(k8, q[part][h][i], s[u]);
+                    if (ACT == S3_BF16) s[u] = mfma_bf16(widen_word(t.k[u][h][i], scale[u]), __builtin_bit_cast(bf16x8, q[h][i]), s[u]);
+                    else s[u] = mfma_f16(widen_word_f16(t.k[u][h][i], scale[u]), __builtin_bit_cast(f16x8, q[h][i]), s[u]);
                 }
             }
         }
-        bool nan = false;
+        if (ACT == S3_F16 || NH > 1) {
+            bool any = false;
 #pragma unroll
-        for (int h = 0; h < T; h++) nan = nan || t.ks[0][h] == 255u || t.ks[1][h] == 255u;
-        if (NH > 1 && __builtin_amdgcn_ballot_w64(nan)) {
-            // a block that reads as NaN must not reach the other heads' columns (NaN times their zeros)
-#pragma unroll
-            for (int u = 0; u < 2; u++)
-#pragma unroll 1
-                for (int sub = 0; sub < heads; sub++) {
-                    f32x4 c = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int h = 0; h < T; h++)
-#pragma unroll
-                        for (int i = 0; i < 4; i++) {
-                            const bool its = k_head(h) == sub;
-                            const bf16x8 k8 = widen_word(its ? t.k[u][h][i] : 0u, its ? fp4_scale(t.ks[u][h]) : 1.f);
-#pragma unroll
-                            for (int part = 0; part < QP; part++) c = mfma_bf16(k8, q[part][h][i], c);
-                        }
-                    if (qsub == sub) s[u] = c;
-                }
+            for (int h = 0; h < T; h++) any = any || special(t.ks[0][h]) || special(t.ks[1][h]);
+            if (__builtin_expect(__builtin_amdgcn_ballot_w64(any) != 0, 0)) special_scores(t, s);
         }
         float p[8];
 #pragma unroll
@@ -421,19 +449,22 @@ struct Fp4Wave {
         }
     }
 
-    // A decode step's new row, still 16-bit, as the last of a tile's `rows` rows: its blocks are rounded by the lanes that use them and
-    // written to the arena (row `row`) by those that own the bytes.
-    __device__ __forceinline__ void take_new_row(Fp4Tile<W> &t, int b, int64_t row, int rows) const {
-        const int64_t at = row * code_bytes, scale_at = row * scale_bytes;
-        const int present = heads * D, kbase = kh0 * D;  // elements of the unit that there are, of the row in front of it
-        const char *k_new = a.k_new + ((int64_t)b * a.H * D + kbase) * 2, *v_new = a.v_new + ((int64_t)b * a.H * D + kbase) * 2;
-#pragma unroll
-        for (int h = 0; h < T; h++) {
+    // A decode step's new row, still 16-bit, as the last of `rows` rows of a tile whose loads have arrived: its blocks are rounded, written
+    // to the arena (row `row`), and put in the places of the tile's rows from rows - 1 on, which hold what the arena held there.  A lane
+    // has a block of K and one of V.
+    __device__ __forceinline__ void take_new_row(char *stage, int b, int64_t row, int rows) const {
+        constexpr int LPR = 64 / Ring::PER_LOAD;
+        const int first = lane / LPR, piece = lane % LPR, pieces = heads * (D / 32);
+        const int mine = piece < pieces ? piece : piece & (D / 32 - 1), base = kh0 * D + mine * 32;  // first element within the row
+        const int shift = W > D * NH ? 2 * (kh0 & 1) : 0;
+#pragma unroll 1
+        for (int which = 0; which < 2; which++) {
+            const char *src = (which ? a.v_new : a.k_new) + ((int64_t)b * a.H * D + base) * 2;
             float x[4][8];
             unsigned most = 0;
 #pragma unroll
             for (int i = 0; i < 4; i++) {
-                widen8<ACT>(*(const u32x4 *)(k_new + k_element(h) * 2 + i * 16), x[i]);
+                widen8<ACT>(*(const u32x4 *)(src + i * 16), x[i]);
 #pragma unroll
                 for (int e = 0; e < 8; e++) most = fp4_magnitude(x[i][e], most);
             }
@@ -441,45 +472,23 @@ struct Fp4Wave {
             u32x4 c;
 #pragma unroll
             for (int i = 0; i < 4; i++) c[i] = fp4_codes8(x[i], byte);
-            if (r == 0 && h * 128 + g * 32 < present) {
-                *(u32x4 *)(a.kplane + at + (kbase + k_element(h)) / 2) = c;
-                a.kscale[scale_at + (kbase + k_element(h)) / 32] = (char)byte;
+            char *scales = (which ? a.vscale : a.kscale) + row * scale_bytes;
+            if (first == 0 && piece < pieces) {
+                *(u32x4 *)((which ? a.vplane : a.kplane) + row * code_bytes + base / 2) = c;
+                scales[base / 32] = (char)byte;
             }
+            const int used = a.H * (D / 32);
+            if (kh0 + NH >= a.H && lane < scale_bytes - used) scales[used + lane] = 0;  // zeros up to a multiple of 16 bytes
+            char *tile = stage + which * 32 * Ring::ROW, *s = stage + 64 * Ring::ROW + which * 128 * T;
 #pragma unroll
-            for (int u = 0; u < 2; u++)
-                if (16 * u + r >= rows - 1) {
-                    t.k[u][h] = c;
-                    t.ks[u][h] = byte;
-                }
+            for (int i = 0; i < Ring::LOADS; i++) {
+                const int place = i * Ring::PER_LOAD + first;
+                const int swap = W == 256 ? (place >> 1) & 7 : (place >> 2) & 3;
+                const int its = which ? (place & 16) + 4 * (place & 3) + ((place >> 2) & 3) : place;
+                if (its >= rows - 1) *(u32x4 *)(tile + place * Ring::ROW + (which ? piece : piece ^ swap) * 16) = c;
+                if (place >= rows - 1 && piece < pieces) s[place * 4 * T + shift + piece] = (char)byte;
+            }
         }
-        const bool v_own = g == 0 && 8 * T * r < present;
-        float x[T][8];
-        unsigned most = 0;
-#pragma unroll
-        for (int h = 0; h < T; h++) {
-            widen8<ACT>(*(const u32x4 *)(v_new + v_element() * 2 + h * 16), x[h]);
-#pragma unroll
-            for (int e = 0; e < 8; e++) most = fp4_magnitude(x[h][e], most);
-        }
-        most = group_max<4 / T>(most);
-        const unsigned byte = fp4_scale_byte<ACT>(__builtin_bit_cast(float, most));
-#pragma unroll
-        for (int h = 0; h < T; h++) {
-            const unsigned c = fp4_codes8(x[h], byte);
-            if (v_own) *(unsigned *)(a.vplane + at + (kbase + v_element()) / 2 + 4 * h) = c;
-#pragma unroll
-            for (int e = 0; e < 8; e++)
-                if (16 * (e >> 2) + 4 * g + (e & 3) >= rows - 1) t.v[e][h] = c;
-        }
-        if (v_own && v_element() % 32 == 0) a.vscale[scale_at + (kbase + v_element()) / 32] = (char)byte;
-        const int used = a.H * (D / 32);
-        if (kh0 + NH >= a.H && lane < scale_bytes - used) {  // zeros up to a multiple of 16 bytes
-            a.kscale[scale_at + used + lane] = 0;
-            a.vscale[scale_at + used + lane] = 0;
-        }
-#pragma unroll
-        for (int e = 0; e < 8; e++)
-            if (16 * (e >> 2) + 4 * g + (e & 3) >= rows - 1) t.vs[e] = byte;
     }
 
     // Four neighbouring elements of this lane's column, i < 2T, rr < 4: elements 8T * (4g + rr) + 4i .. + 3 of the unit.
@@ -553,8 +562,9 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_team_kernel(const AttnArgs a)
             } else {
                 wait_loads<0>();
             }
-            w.read(t, w.ring + (i & 1) * Wave::Ring::STAGE);
-            if (has_new && left <= 32) w.take_new_row(t, it.b, it.off + it.len - 1, left);
+            char *stage = w.ring + (i & 1) * Wave::Ring::STAGE;
+            if (has_new && left <= 32) w.take_new_row(stage, it.b, it.off + it.len - 1, left);
+            w.read(t, stage);
             w.fold(t, left);
         }
 
@@ -779,10 +789,11 @@ __global__ void __launch_bounds__(512, 2) attn_fp4_share_kernel(const AttnArgs a
         if (behind >= 2) wait_loads<2 * Wave::Ring::TILE_LOADS>();
         else if (behind == 1) wait_loads<Wave::Ring::TILE_LOADS>();
         else wait_loads<0>();
-        w.read(t, w.ring + take * Wave::Ring::STAGE);
-        take = take + 1 == DEEP ? 0 : take + 1;
+        char *stage = w.ring + take * Wave::Ring::STAGE;
         const int rows = now.len - (now.tile - now.begin) * 32;
-        if (a.k_new != nullptr && rows <= 32) w.take_new_row(t, now.b, now.off + now.len - 1, rows);
+        if (a.k_new != nullptr && rows <= 32) w.take_new_row(stage, now.b, now.off + now.len - 1, rows);
+        w.read(t, stage);
+        take = take + 1 == DEEP ? 0 : take + 1;
         w.fold(t, rows);
         const int next = now.tile + 1;
         if (next == now.end || next == t1) {
