@@ -4,7 +4,8 @@
 // A head x of D elements is first divided by its root mean square, x * rsqrt(mean(x^2) + eps) * w (if w is given), then its pairs
 // (a, b) turn by the angle t = rot_pos[axis] * inv_freq[pair]: (a cos t - b sin t, a sin t + b cos t).  Per element that is
 // y = inv * (x * cw + x' * sw), where x' is the other element of the pair and cw, sw hold cosine, (signed) sine and norm weight:
-// they depend on the token and the element only, so a wave works them out once and goes through the token's heads with them.
+// they depend on the token and the element only, so a wave works them out once, a pair a lane, and goes through the token's heads with
+// them.
 // All in fp32, rounded once to the type of the output or to the codes of the cache; angles in turns of 64 bits, since a far
 // position times a frequency leaves few bits of the turn in 32.
 //
@@ -113,33 +114,59 @@ template <int ACT, int D, int CACHE, int PAIRS>
 __global__ void __launch_bounds__(256) rotary_kernel(const RotaryArgs a) {
     constexpr int LPH = D == 96 ? 16 : D / 8;  // lanes a head (of 96: twelve of sixteen)
     constexpr int GH = 64 / LPH;               // heads a wave takes at once
+    constexpr int P = (D / 2 + 63) / 64;       // pairs a lane works out
+    __shared__ f32x2 turned[4][64 * P];        // cosine and sine of a wave's token, by pair
     const int lane = threadIdx.x & 63, sub = lane / LPH, e0 = (lane % LPH) * 8;
     const bool lane_ok = D != 96 || e0 < D;
     const int e = lane_ok ? e0 : 0;
+    f32x2 *mine = turned[__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)];
     const int64_t row_bytes = CACHE == S3_ROT_MXFP4 ? fp4_code_bytes(a.Hkv, D) : (int64_t)a.Hkv * D * (CACHE == S3_ROT_E4M3 ? 1 : 2);
     const int half = a.rotary / 2;
-    // this lane's elements: turns per position, axis and other element of the pair, whatever the token
-    double rate[8];
-    int mine[8], other[8];
-    unsigned axis = 0;
+    // turns per position and axis of the lane's pairs, whatever the token
+    double rate[P];
+    int axis[P];
+#pragma unroll
+    for (int i = 0; i < P; i++) {
+        const int pair = lane + 64 * i;
+        rate[i] = pair < half ? (double)a.inv_freq[pair] * 0.15915494309189533577 : 0.0;
+        axis[i] = (int)(a.axes[(pair >> 5) & 3] >> (2 * (pair & 31))) & 3;
+    }
+    // the lane's elements: the pair of the first, which half of its pair it is, and where the other elements are
+    const bool second = e >= half;  // (PAIRS 1: of all eight)
+    int at[8], other[8];
 #pragma unroll
     for (int i = 0; i < 8; i++) {
         const int el = e + i;
-        const bool second = PAIRS == 0 ? el & 1 : el >= half;
-        const int pair = PAIRS == 0 ? el >> 1 : second ? el - half : el;
-        rate[i] = 0.0;
-        mine[i] = other[i] = el;
-        if (el < a.rotary) {
-            rate[i] = (double)a.inv_freq[pair] * 0.15915494309189533577;
-            axis |= (unsigned)((a.axes[pair >> 5] >> (2 * (pair & 31))) & 3) << (2 * i);
-            other[i] = PAIRS == 0 ? el ^ 1 : second ? el - half : el + half;
-        }
+        const bool turns = el < a.rotary;
+        at[i] = !turns ? 0 : PAIRS == 0 ? el >> 1 : el >= half ? el - half : el;
+        other[i] = !turns ? el : PAIRS == 0 ? el ^ 1 : el >= half ? el - half : el + half;
     }
-    const int gq = (a.Hq + GH - 1) / GH, gk = (a.Hkv + GH - 1) / GH;
+    const int gq = (a.Hq + GH - 1) / GH, gk = (a.Hkv + GH - 1) / GH, groups = gq + gk + (CACHE == S3_ROT_NONE ? 0 : gk);
     const unsigned lane_at = (unsigned)(sub * D + e) * 2, other_at = (unsigned)(sub * D + other[0]) * 2;
     for (int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); item < (int64_t)a.n * a.parts; item += (int64_t)gridDim.x * 4) {
         const int64_t t = uniform64(a.parts == 1 ? item : item / a.parts);
         const int part = __builtin_amdgcn_readfirstlane((int)(item - t * a.parts));
+        // this wave's groups of heads: part, part + parts, ... of the queries', the keys' and the values'
+        u32x4 raw, raw_other = {0u, 0u, 0u, 0u};
+        unsigned short one[8];
+        const auto load = [&](int x) {
+            const char *src = x < gq ? a.q + t * a.q_step + (int64_t)x * (GH * D * 2)
+                            : x < gq + gk ? a.k + t * a.k_step + (int64_t)(x - gq) * (GH * D * 2)
+                                          : a.v + t * a.v_step + (int64_t)(x - gq - gk) * (GH * D * 2);
+            const int left = x < gq ? a.Hq - x * GH : a.Hkv - (x < gq + gk ? x - gq : x - gq - gk) * GH;
+            raw = (u32x4){0u, 0u, 0u, 0u};
+            if (lane_ok && sub < left) {
+                raw = *(const u32x4 *)(src + lane_at);
+                if (x < gq + gk) {
+                    if (PAIRS == 1) raw_other = *(const u32x4 *)(src + other_at);
+                    if (PAIRS == 2) {
+#pragma unroll
+                        for (int i = 0; i < 8; i++) one[i] = *(const unsigned short *)(src + (unsigned)(sub * D + other[i]) * 2);
+                    }
+                }
+            }
+        };
+        load(part);
         int64_t row = 0, scale = 0;  // bytes into the planes
         int32_t p = 0;
         if (CACHE != S3_ROT_NONE) {
@@ -150,114 +177,100 @@ __global__ void __launch_bounds__(256) rotary_kernel(const RotaryArgs a) {
             scale = CACHE == S3_ROT_MXFP4 ? (off + p) * fp4_scale_bytes(a.Hkv, D) : 0;
         }
         float cs[8], sn[8];
-        {
-            int32_t at[4];
+        if (half > 0 && part < gq + gk) {
+            int32_t where[4];
 #pragma unroll
-            for (int x = 0; x < 4; x++) at[x] = a.rot_pos && a.rotary ? a.rot_pos[(int64_t)min(x, a.n_axes - 1) * a.n + t] : p;
+            for (int x = 0; x < 4; x++) where[x] = a.rot_pos ? a.rot_pos[(int64_t)min(x, a.n_axes - 1) * a.n + t] : p;
+#pragma unroll
+            for (int i = 0; i < P; i++) {
+                double turn = (double)(axis[i] & 2 ? axis[i] & 1 ? where[3] : where[2] : axis[i] & 1 ? where[1] : where[0]) * rate[i];
+                turn -= rint(turn);
+                float s, c;
+                sin_cos_turn((float)turn, s, c);
+                mine[lane + 64 * i] = (f32x2){c, s};
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                const unsigned ax = (axis >> (2 * i)) & 3;
-                double turn = (double)(ax & 2 ? ax & 1 ? at[3] : at[2] : ax & 1 ? at[1] : at[0]) * rate[i];
-                turn -= rint(turn);
-                sin_cos_turn((float)turn, sn[i], cs[i]);
-                const bool second = PAIRS == 0 ? i & 1 : e + i >= half;
-                if (!second) sn[i] = -sn[i];  // (elements that do not turn: no angle, cosine 1, sine 0)
+                const f32x2 v = PAIRS == 1 ? mine[at[0] + i] : mine[at[i]];
+                const bool turns = (PAIRS == 1 ? e : e + i) < a.rotary;
+                const bool b = PAIRS == 0 ? i & 1 : PAIRS == 1 ? second : e + i >= half;
+                cs[i] = turns ? v[0] : 1.f;
+                sn[i] = turns ? b ? v[1] : -v[1] : 0.f;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                cs[i] = 1.f;
+                sn[i] = 0.f;
             }
         }
-        // heads of one kind, GH at a time, this wave's share of them: first, first + parts, ...; put(h, bytes from the head's row, y)
-        auto turn_heads = [&](const char *src, int heads, int groups, int before, const float *weight, auto &&put) {
-            int hg = part - before % a.parts;
-            if (hg < 0) hg += a.parts;
-            if (hg >= groups) return;
-            float cw[8], sw[8];
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                cw[i] = cs[i];
-                sw[i] = sn[i];
-            }
-            if (weight) {
-                float w[8], wo[8];
-                load_weight8<true>(weight, mine, w);
-                if (PAIRS == 0) {
-#pragma unroll
-                    for (int i = 0; i < 8; i++) wo[i] = w[i ^ 1];
-                } else {
-                    load_weight8<PAIRS == 1>(weight, other, wo);
-                }
+        float cw[8], sw[8];
+        int kind = -1;  // of the heads at hand: queries, keys, values
+        for (int x = part; x < groups; x += a.parts) {
+            const int now = x < gq ? 0 : x < gq + gk ? 1 : 2, heads = now == 0 ? a.Hq : a.Hkv;
+            const int h = (now == 0 ? x : now == 1 ? x - gq : x - gq - gk) * GH + sub;
+            const float *weight = now == 0 ? a.q_weight : a.k_weight;
+            if (now != kind && now < 2) {
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
-                    cw[i] *= w[i];
-                    sw[i] *= wo[i];
+                    cw[i] = cs[i];
+                    sw[i] = sn[i];
                 }
-            }
-            u32x4 raw, raw_other = {0u, 0u, 0u, 0u};
-            unsigned short one[8];
-            auto load = [&](int group) {
-                const char *at = src + (int64_t)group * (GH * D * 2);
-                const bool ok = lane_ok && group * GH + sub < heads;
-                raw = (u32x4){0u, 0u, 0u, 0u};
-                if (ok) {
-                    raw = *(const u32x4 *)(at + lane_at);
-                    if (PAIRS == 1) raw_other = *(const u32x4 *)(at + other_at);
-                    if (PAIRS == 2) {
+                if (weight) {
+                    float w[8], wo[8];
+                    const int first[8] = {e, e + 1, e + 2, e + 3, e + 4, e + 5, e + 6, e + 7};
+                    load_weight8<true>(weight, first, w);
+                    if (PAIRS == 0) {
 #pragma unroll
-                        for (int i = 0; i < 8; i++) one[i] = *(const unsigned short *)(at + (unsigned)(sub * D + other[i]) * 2);
+                        for (int i = 0; i < 8; i++) wo[i] = w[i ^ 1];
+                    } else {
+                        load_weight8<PAIRS == 1>(weight, other, wo);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; i++) {
+                        cw[i] *= w[i];
+                        sw[i] *= wo[i];
                     }
                 }
-            };
-            load(hg);
-            while (true) {
-                float x[8], xo[8], y[8];
-                widen8<ACT>(raw, x);
-                if (PAIRS == 1) widen8<ACT>(raw_other, xo);
-#pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    if (PAIRS == 0) xo[i] = x[i ^ 1];
-                    if (PAIRS == 2) xo[i] = widen16<ACT>(one[i]);
-                }
-                const int h = hg * GH + sub;
-                hg += a.parts;
-                const bool more = hg < groups;
-                if (more) load(hg);  // the next heads are on their way while these are turned
-                float inv = 1.f;
-                if (weight) {
-                    float sum = 0.f;
-#pragma unroll
-                    for (int i = 0; i < 8; i++) sum = fmaf(x[i], x[i], sum);
-                    sum = group_sum<LPH>(sum);
-                    inv = 1.f / sqrtf(sum * (1.f / D) + a.eps);
-                }
-#pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    // (elements that do not turn: infinities times a sine of 0 are kept out)
-                    const float its = (PAIRS == 1 ? e : e + i) < a.rotary ? xo[i] * inv * sw[i] : 0.f;
-                    y[i] = fmaf(x[i] * inv, cw[i], its);
-                }
-                if (lane_ok && h < heads) put(h, y);
-                if (!more) break;
             }
-        };
-        turn_heads(a.q + t * a.q_step, a.Hq, gq, 0, a.q_weight, [&](int h, const float (&y)[8]) {
-            *(u32x4 *)(a.q_out + t * a.q_out_step + (h * D + e) * 2) = round8<ACT>(y);
-        });
-        turn_heads(a.k + t * a.k_step, a.Hkv, gk, gq, a.k_weight, [&](int h, const float (&y)[8]) {
-            if (CACHE == S3_ROT_NONE) *(u32x4 *)(a.k_out + t * a.k_out_step + (h * D + e) * 2) = round8<ACT>(y);
+            kind = now;
+            const u32x4 bits = raw;
+            float v[8], vo[8], y[8];
+            widen8<ACT>(raw, v);
+            if (PAIRS == 1) widen8<ACT>(raw_other, vo);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                if (PAIRS == 0) vo[i] = v[i ^ 1];
+                if (PAIRS == 2) vo[i] = widen16<ACT>(one[i]);
+            }
+            if (x + a.parts < groups) load(x + a.parts);  // the next heads are on their way while these are turned
+            const bool ok = lane_ok && h < heads;
+            if (now == 2) {
+                if (!ok) continue;
+                if (CACHE == S3_ROT_16BIT) *(u32x4 *)(a.vplane + row + (h * D + e) * 2) = bits;
+                else store_row8<ACT, D, CACHE>(a.vplane + row, a.vscale + scale, a.Hkv, h, e, v);
+                continue;
+            }
+            float inv = 1.f;
+            if (weight) {
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; i++) sum = fmaf(v[i], v[i], sum);
+                sum = group_sum<LPH>(sum);
+                inv = 1.f / sqrtf(sum * (1.f / D) + a.eps);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                // (elements that do not turn: infinities times a sine of 0 are kept out)
+                const float its = (PAIRS == 1 ? e : e + i) < a.rotary ? vo[i] * inv * sw[i] : 0.f;
+                y[i] = fmaf(v[i] * inv, cw[i], its);
+            }
+            if (!ok) continue;
+            if (now == 0) *(u32x4 *)(a.q_out + t * a.q_out_step + (h * D + e) * 2) = round8<ACT>(y);
+            else if (CACHE == S3_ROT_NONE) *(u32x4 *)(a.k_out + t * a.k_out_step + (h * D + e) * 2) = round8<ACT>(y);
             else store_row8<ACT, D, CACHE>(a.kplane + row, a.kscale + scale, a.Hkv, h, e, y);
-        });
-        if (CACHE != S3_ROT_NONE) {
-            int hg = part - (gq + gk) % a.parts;
-            for (hg = hg < 0 ? hg + a.parts : hg; hg < gk; hg += a.parts) {
-                const int h = hg * GH + sub;
-                if (!lane_ok || h >= a.Hkv) continue;
-                const u32x4 raw = *(const u32x4 *)(a.v + t * a.v_step + (int64_t)hg * (GH * D * 2) + lane_at);
-                if (CACHE == S3_ROT_16BIT) {
-                    *(u32x4 *)(a.vplane + row + (h * D + e) * 2) = raw;
-                } else {
-                    float x[8];
-                    widen8<ACT>(raw, x);
-                    store_row8<ACT, D, CACHE>(a.vplane + row, a.vscale + scale, a.Hkv, h, e, x);
-                }
-            }
         }
     }
 }
