@@ -23,6 +23,7 @@ LIB_PATH = os.environ.get("S3KV_LIB") or os.path.join(_HERE, "libs3kv.so")  # S3
 CALL_PATH = os.path.join(_HERE, "_s3call" + sysconfig.get_config_var("EXT_SUFFIX"))  # compiled for one interpreter
 _lib = None
 _call = None  # the extension module of the per-layer calls, connected to the loaded library
+_rows = None  # the same module, once its calls around an append are connected too
 
 
 class s3_kv_config(ctypes.Structure):
@@ -112,6 +113,15 @@ def _connect():
     module.connect(ctypes.c_void_p, *[ctypes.cast(getattr(handle, f), ctypes.c_void_p).value
                                       for f in ("s3_decode_step", "s3_decode_step_static", "s3_kv_append", "s3_decode_attention", "s3_kv_fill_batch")])
     _call = module
+    return module
+
+
+def _connect_rows():
+    """The call path of the calls around an append (s3_kv_append_rotary, s3_qk_rotary, s3_kv_fetch)."""
+    global _rows
+    module, handle = _call or _connect(), lib()
+    module.connect_rows(*[ctypes.cast(getattr(handle, f), ctypes.c_void_p).value for f in ("s3_kv_append_rotary", "s3_qk_rotary", "s3_kv_fetch")])
+    _rows = module
     return module
 
 
@@ -225,12 +235,22 @@ def _rule(rule):
 
 
 def s3_qk_rotary(rule, dtype, head_dim, n, rot_pos, q, n_heads, k, n_kv_heads, q_out, k_out, q_stride=0, k_stride=0, stream=0):
+    if type(rule) is s3_rotary:
+        st = (_rows or _connect_rows()).qk_rotary(ctypes.addressof(rule), dtype, head_dim, n, rot_pos, q, n_heads, q_stride, k, n_kv_heads,
+                                                  k_stride, q_out, k_out, stream)
+        if st is not None:
+            return st
     return lib().s3_qk_rotary(_rule(rule), int(dtype), int(head_dim), int(n), _ptr(rot_pos), _ptr(q), int(n_heads), int(q_stride), _ptr(k),
                               int(n_kv_heads), int(k_stride), _ptr(q_out), _ptr(k_out), stream or None)
 
 
 def s3_kv_append_rotary(arena, layer, n, slot_off, pos, rule, q, k_new, v_new, q_out, rot_pos=None, q_stride=0, k_stride=0, v_stride=0,
                         stream=0, slot_id=None, pos_host=None):
+    if slot_id is None and pos_host is None and type(rule) is s3_rotary:
+        st = (_rows or _connect_rows()).append_rotary(arena, layer, n, slot_off, pos, ctypes.addressof(rule), rot_pos, q, q_stride, k_new,
+                                                      k_stride, v_new, v_stride, q_out, stream)
+        if st is not None:
+            return st
     _a, idp = _host_i32(slot_id)
     _b, php = _host_i32(pos_host)
     return lib().s3_kv_append_rotary(arena, int(layer), int(n), idp, php, _ptr(slot_off), _ptr(pos), _rule(rule), _ptr(rot_pos), _ptr(q),
@@ -238,6 +258,9 @@ def s3_kv_append_rotary(arena, layer, n, slot_off, pos, rule, q, k_new, v_new, q
 
 
 def s3_kv_fetch(arena, layer, n, slot_off, pos, k_out, v_out, stream=0):
+    st = (_rows or _connect_rows()).fetch(arena, layer, n, slot_off, pos, k_out, v_out, stream)
+    if st is not None:
+        return st
     return lib().s3_kv_fetch(arena, int(layer), int(n), _ptr(slot_off), _ptr(pos), _ptr(k_out), _ptr(v_out), stream or None)
 
 

@@ -17,7 +17,16 @@ typedef int (*attention_fn)(void *, int32_t, int32_t, const void *, const void *
 typedef int (*fill_fn)(void *, int32_t, int32_t, const int32_t *, const int32_t *, void **, void **, int32_t, void *, void *, const int32_t *,
                        void *);
 
+typedef int (*append_rotary_fn)(void *, int32_t, int32_t, const int32_t *, const int32_t *, const void *, const void *, const void *, const void *,
+                                const void *, int64_t, const void *, int64_t, const void *, int64_t, void *, void *);
+typedef int (*qk_rotary_fn)(const void *, int32_t, int32_t, int32_t, const void *, const void *, int32_t, int64_t, const void *, int32_t, int64_t,
+                            void *, void *, void *);
+typedef int (*fetch_fn)(void *, int32_t, int32_t, const void *, const void *, void *, void *, void *);
+
 static step_fn g_step, g_static;
+static append_rotary_fn g_append_rotary;
+static qk_rotary_fn g_qk_rotary;
+static fetch_fn g_fetch;
 static fill_fn g_fill;
 static append_fn g_append;
 static attention_fn g_attention;
@@ -60,6 +69,12 @@ static int handle(PyObject *x, void **out) {
 static int number(PyObject *x, int32_t *out) {
     if (!PyLong_Check(x)) return 0;
     *out = (int32_t)PyLong_AsUnsignedLongMask(x);
+    return PyErr_Occurred() ? -1 : 1;
+}
+
+static int number64(PyObject *x, int64_t *out) {
+    if (!PyLong_Check(x)) return 0;
+    *out = (int64_t)PyLong_AsUnsignedLongLongMask(x);
     return PyErr_Occurred() ? -1 : 1;
 }
 
@@ -190,6 +205,72 @@ static PyObject *fill(PyObject *, PyObject *const *a, Py_ssize_t count) {
     return PyLong_FromLong(rc);
 }
 
+// (arena, layer, n, slot_off, pos, rule's address, rot_pos, q, q_stride, k_new, k_stride, v_new, v_stride, q_out, stream)
+static PyObject *append_rotary(PyObject *, PyObject *const *a, Py_ssize_t count) {
+    if (!g_append_rotary || count != 15) Py_RETURN_NONE;
+    void *arena, *p[8], *stream;
+    int64_t stride[3];
+    int32_t layer, n;
+    TAKE(handle(a[0], &arena));
+    TAKE(number(a[1], &layer));
+    TAKE(number(a[2], &n));
+    static const int pointers[8] = {3, 4, 5, 6, 7, 9, 11, 13};
+    for (int i = 0; i < 8; i++) TAKE(address(a[pointers[i]], &p[i]));
+    for (int i = 0; i < 3; i++) TAKE(number64(a[8 + 2 * i], &stride[i]));
+    TAKE(stream_of(a[14], &stream));
+    int rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = g_append_rotary(arena, layer, n, nullptr, nullptr, p[0], p[1], p[2], p[3], p[4], stride[0], p[5], stride[1], p[6], stride[2], p[7], stream);
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(rc);
+}
+
+// (rule's address, dtype, head_dim, n, rot_pos, q, n_heads, q_stride, k, n_kv_heads, k_stride, q_out, k_out, stream)
+static PyObject *qk_rotary(PyObject *, PyObject *const *a, Py_ssize_t count) {
+    if (!g_qk_rotary || count != 14) Py_RETURN_NONE;
+    void *p[6], *stream;
+    int64_t stride[2];
+    int32_t v[5];
+    static const int pointers[6] = {0, 4, 5, 8, 11, 12}, plain[5] = {1, 2, 3, 6, 9};
+    for (int i = 0; i < 6; i++) TAKE(address(a[pointers[i]], &p[i]));
+    for (int i = 0; i < 5; i++) TAKE(number(a[plain[i]], &v[i]));
+    TAKE(number64(a[7], &stride[0]));
+    TAKE(number64(a[10], &stride[1]));
+    TAKE(stream_of(a[13], &stream));
+    int rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = g_qk_rotary(p[0], v[0], v[1], v[2], p[1], p[2], v[3], stride[0], p[3], v[4], stride[1], p[4], p[5], stream);
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(rc);
+}
+
+// (arena, layer, n, slot_off, pos, k_out, v_out, stream)
+static PyObject *fetch(PyObject *, PyObject *const *a, Py_ssize_t count) {
+    if (!g_fetch || count != 8) Py_RETURN_NONE;
+    void *arena, *p[4], *stream;
+    int32_t layer, n;
+    TAKE(handle(a[0], &arena));
+    TAKE(number(a[1], &layer));
+    TAKE(number(a[2], &n));
+    for (int i = 0; i < 4; i++) TAKE(address(a[3 + i], &p[i]));
+    TAKE(stream_of(a[7], &stream));
+    int rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = g_fetch(arena, layer, n, p[0], p[1], p[2], p[3], stream);
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(rc);
+}
+
+// (the addresses of s3_kv_append_rotary, s3_qk_rotary and s3_kv_fetch of the loaded library)
+static PyObject *connect_rows(PyObject *, PyObject *args) {
+    unsigned long long r, q, f;
+    if (!PyArg_ParseTuple(args, "KKK", &r, &q, &f)) return nullptr;
+    g_append_rotary = (append_rotary_fn)(uintptr_t)r;
+    g_qk_rotary = (qk_rotary_fn)(uintptr_t)q;
+    g_fetch = (fetch_fn)(uintptr_t)f;
+    Py_RETURN_NONE;
+}
+
 // (ctypes.c_void_p, then the addresses of s3_decode_step, s3_decode_step_static, s3_kv_append, s3_decode_attention and
 // s3_kv_fill_batch of the loaded library)
 static PyObject *connect(PyObject *, PyObject *args) {
@@ -213,6 +294,10 @@ static PyMethodDef methods[] = {
     {"append", (PyCFunction)(void (*)())append, METH_FASTCALL, nullptr},
     {"attention", (PyCFunction)(void (*)())attention, METH_FASTCALL, nullptr},
     {"fill", (PyCFunction)(void (*)())fill, METH_FASTCALL, nullptr},
+    {"connect_rows", connect_rows, METH_VARARGS, nullptr},
+    {"append_rotary", (PyCFunction)(void (*)())append_rotary, METH_FASTCALL, nullptr},
+    {"qk_rotary", (PyCFunction)(void (*)())qk_rotary, METH_FASTCALL, nullptr},
+    {"fetch", (PyCFunction)(void (*)())fetch, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 static PyModuleDef module = {PyModuleDef_HEAD_INIT, "_s3call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
