@@ -1000,6 +1000,7 @@ append_fp8_fn s3i_pick_append_fp8(int act);
 // Kernels for rows of 4-bit blocks (defined in s3kv_fp4.hip): attention for new rows and queries of type act (256 threads; wide_out:
 // 32-bit outputs; heads_per_unit: 2 for pairs of heads of 64; shares: equal shares of all rows, or chunks of contexts; lds: bytes of it behind
 // the batch view) and the append that rounds a new row.
+#define S3_FP4_KNOWN 1024  // contexts up to which attn_fp4_share_kernel keeps offsets and rows in LDS
 attn_fn s3i_pick_fp4(int act, int d, int heads_per_unit, bool wide_out, bool shares, int *lds);
 typedef void (*append_fp4_fn)(const AttnArgs);  // kplane .. vscale, slot_off, cur_len, k_new, v_new, n_tokens, H * D in `columns`, max_len
 append_fp4_fn s3i_pick_append_fp4(int act);

@@ -332,6 +332,15 @@ struct Fp4Wave {
         for (int i = 0; i < 8 * T; i++) acc[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
 
+    // Asks for the queries of a context to come, so that begin() finds them in L2: a word of every 64 bytes, into 256 bytes of LDS that
+    // nobody reads.
+    __device__ __forceinline__ void touch_queries(char *nowhere, int b) const {
+        const int head = column ? qhead : kh0 * a.group + qb * QB;
+#pragma unroll
+        for (int h = 0; h < (D == 256 ? 2 : 1); h++)
+            __builtin_amdgcn_global_load_lds((glb_void *)(a.q + (((int64_t)b * a.Hq + head) * D + (h * 128 + g * 32) % D) * 2), (lds_void *)nowhere, 4, 0, 0);
+    }
+
     // Blocks that the products of fold() do not take: with several heads, those that read as NaN, which must not reach the other heads'
     // columns (NaN times their zeros); beside fp16 queries, those with a scale under which a code is no fp16 number (appended rows have
     // none: their scales are 101 to 140, or 1 for a block of zeros, and a scale below 104 only where no code is odd).
@@ -501,6 +510,73 @@ struct Fp4Wave {
         }
         return o;
     }
+
+    // This lane's first element of its column's head (32T from there on are its own), and whether it has any.
+    __device__ __forceinline__ int first_element() const { return 32 * T * g - D * qsub; }
+    __device__ __forceinline__ bool delivers() const { return column && first_element() >= 0 && first_element() < D; }
+
+    // The output rows of context b for this column; total: the weights' sum of the lane's column.
+    __device__ __forceinline__ void deliver(int b, const float total) const {
+        const float inv = 1.f / total;
+        if (!delivers()) return;
+#pragma unroll
+        for (int rr = 0; rr < 4; rr++)
+#pragma unroll
+            for (int i = 0; i < T; i++) {
+                const f32x4 lo = sums4(rr, 2 * i), hi = sums4(rr, 2 * i + 1);
+                const float o[8] = {lo[0] * inv, lo[1] * inv, lo[2] * inv, lo[3] * inv, hi[0] * inv, hi[1] * inv, hi[2] * inv, hi[3] * inv};
+                store_out8(a.out, a.out_dtype, ((int64_t)b * a.Hq + qhead) * D + first_element() + 8 * T * rr + 8 * i, o);
+            }
+    }
+
+    // A piece of a context, as the lanes hold it: 8T quads a lane, lanes that deliver side by side, so that a store covers whole lines
+    // (written a row of the output at a time, 16 bytes here and there past the caches, the pieces of 1024 contexts of 512 rows, 16q/1kv x
+    // 256, took as long as their rows: 75 us).
+    __device__ __forceinline__ unsigned piece_lane() const {
+        return ((qsub * per_head + r % QB) * (D / (32 * T)) + first_element() / (32 * T)) * 16;
+    }
+    __device__ __forceinline__ unsigned piece_quads() const { return heads * per_head * (D / (32 * T)) * 16; }  // bytes of one quad of all lanes
+    __device__ __forceinline__ float *piece(int64_t slot) const { return a.part_acc + (slot * a.Hq + kh0 * a.group + qb * QB) * D; }
+    __device__ __forceinline__ void put_piece(int64_t slot, const float total) const {
+        if (!delivers()) return;
+        if (first_element() == 0) put_partial2<true>((float *)a.part_ml + 2 * (slot * a.Hq + qhead), (f32x2){m, total});
+        char *to = (char *)piece(slot) + piece_lane();
+#pragma unroll
+        for (int i = 0; i < 8 * T; i++) put_partial4<true>((float *)(to + i * piece_quads()), acc[i]);
+    }
+    // Merges the `count` pieces of context b in slots slot0, slot0 + 1, ..., two a memory round trip, and delivers its rows.
+    __device__ __forceinline__ void merge_pieces(int64_t slot0, int b, int count) {
+        m = -INFINITY;
+        l = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8 * T; i++) acc[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        const unsigned bytes = heads * per_head * D * 4, at = delivers() ? piece_lane() : bytes;  // (past the end: zeros, no traffic)
+        for (int c0 = 0; c0 < count; c0 += 2) {
+            f32x2 ml[2];
+            f32x4 p[2][8 * T];
+#pragma unroll
+            for (int u = 0; u < 2; u++) {
+                const int64_t slot = slot0 + c0 + u;
+                const bool is = c0 + u < count;
+                const __amdgpu_buffer_rsrc_t mr = piece_buffer((const float *)a.part_ml + 2 * slot * a.Hq, is ? a.Hq * 8 : 0);
+                const __amdgpu_buffer_rsrc_t pr = piece_buffer(piece(slot), is ? bytes : 0);
+                ml[u] = piece_load2(mr, delivers() ? qhead * 8 : a.Hq * 8);
+#pragma unroll
+                for (int i = 0; i < 8 * T; i++) p[u][i] = piece_load4(pr, at + i * piece_quads());
+            }
+#pragma unroll
+            for (int u = 0; u < 2; u++) {
+                if (c0 + u >= count) break;
+                const float pm = ml[u][0], mn = fmaxf(m, pm), ref = exp_reference(mn);
+                const float old = fast_exp2(m - ref), now = fast_exp2(pm - ref);
+                l = l * old + ml[u][1] * now;
+#pragma unroll
+                for (int i = 0; i < 8 * T; i++) acc[i] = acc[i] * old + p[u][i] * now;
+                m = mn;
+            }
+        }
+        deliver(b, l);
+    }
 };
 
 // The new lengths, and a zero output row for empty or refused contexts, by the workgroups in turn.
@@ -640,7 +716,8 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_team_kernel(const AttnArgs a)
 
 // Exclusive prefix sums of the contexts' tiles into pre[0..n], by the whole workgroup; returns the total (longest: the rows of the
 // longest context).
-__device__ __forceinline__ int tile_prefix(const AttnArgs &a, int *pre, int *wave_sums, int &longest) {
+// off_s, len_s: receive the contexts' offsets and rows, unless off_s is null.
+__device__ __forceinline__ int tile_prefix(const AttnArgs &a, int *pre, int64_t *off_s, int *len_s, int *wave_sums, int &longest) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, nwaves = blockDim.x >> 6;
     constexpr int E = 4;
     int total = 0;
@@ -667,7 +744,13 @@ __device__ __forceinline__ int tile_prefix(const AttnArgs &a, int *pre, int *wav
 #pragma unroll
         for (int e = 0; e < E; e++) {
             const int b = base + tid * E + e;
-            if (b < a.n) pre[b] = run;
+            if (b < a.n) {
+                pre[b] = run;
+                if (off_s) {
+                    off_s[b] = off[e];
+                    len_s[b] = len[e];
+                }
+            }
             run += (len[e] + 31) >> 5;
         }
         if (tid == 0) pre[a.n] = total;
@@ -683,16 +766,19 @@ __device__ __forceinline__ int tile_prefix(const AttnArgs &a, int *pre, int *wav
 // Contexts of few tiles are not cut: a share takes those that begin in it.
 #define S3_FP4_UNCUT 8
 template <int ACT, int D, int NH, int NP>
-__global__ void __launch_bounds__(512, 2) attn_fp4_share_kernel(const AttnArgs a) {
+__device__ __forceinline__ void fp4_share(const AttnArgs &a) {
     typedef Fp4Wave<ACT, D, NH, NP> Wave;
-    constexpr int W = Wave::W, T = Wave::T, QB = Wave::QB;
-    extern __shared__ __align__(16) char dyn_lds[];  // tiles in front of every context, [n + 1]; the waves' rings
+    constexpr int W = Wave::W;
+    extern __shared__ __align__(16) char dyn_lds[];  // the waves' rings; tiles in front of every context, [n + 1]; offsets and rows
     __shared__ int wave_sums[2 * S3_MAX_WAVES];
-    int *pre = (int *)dyn_lds;
-    char *rings = dyn_lds + (((a.n + 1) * 4 + 15) & ~15);
+    constexpr int DEEP = Wave::Ring::DEEP;
+    char *rings = dyn_lds;
+    int *pre = (int *)(dyn_lds + 8 * DEEP * Wave::Ring::STAGE + 8 * 256);
+    const bool known = a.n <= S3_FP4_KNOWN;  // offsets and rows of the contexts are in LDS too
+    int64_t *off_s = (int64_t *)((char *)pre + (((a.n + 1) * 4 + 15) & ~15));
+    int *len_s = (int *)(off_s + a.n);
     int longest = 0;
-    const int total = tile_prefix(a, pre, wave_sums, longest);
-    publish_lengths<D>(a);
+    const int total = tile_prefix(a, pre, known ? off_s : nullptr, len_s, wave_sums, longest);
     const int ts = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // Neighbouring columns, whose bytes share cache lines, are on neighbouring waves, and those on one XCD (workgroup b is on XCD b % 8).
     const int rank = (gridDim.x & 7) == 0 ? (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3) : blockIdx.x;
@@ -709,7 +795,6 @@ __global__ void __launch_bounds__(512, 2) attn_fp4_share_kernel(const AttnArgs a
         if (t0 >= t1) return;
         t1 = __builtin_amdgcn_readfirstlane(pre[find_sequence(pre, a.n, t1 - 1) + 1]);
     }
-    constexpr int DEEP = Wave::Ring::DEEP;
     Wave w(a, rings + ts * DEEP * Wave::Ring::STAGE);
     w.set_column(col);
     Pending head = {0, 0, 0}, tail = {0, 0, 0};  // pieces of the contexts that the share's borders cut
@@ -727,42 +812,27 @@ __global__ void __launch_bounds__(512, 2) attn_fp4_share_kernel(const AttnArgs a
             c.b++;
         }
         c.begin = __builtin_amdgcn_readfirstlane(pre[c.b]);
-        c.off = uniform64(a.slot_off[c.b]);
-        c.len = __builtin_amdgcn_readfirstlane(a.cur_len[c.b]) + a.len_add;  // (a context with tiles: it has been checked)
+        if (known) {
+            c.off = uniform64(off_s[c.b]);
+            c.len = __builtin_amdgcn_readfirstlane(len_s[c.b]);
+        } else {  // (a context with tiles: it has been checked)
+            c.off = uniform64(a.slot_off[c.b]);
+            c.len = __builtin_amdgcn_readfirstlane(a.cur_len[c.b]) + a.len_add;
+        }
         c.tile = tile;
     };
     const auto finish = [&](const Cursor &c) {  // the share's part of context c.b is folded in
         const int first = max(c.begin, t0), last = min(c.end, t1);
         const float l = sum_over_rows(w.l);
-        const int e0 = 32 * T * w.g - D * w.qsub;  // this lane's first element, of its column's head
-        const bool mine = w.column && e0 >= 0 && e0 < D;
         if (first == c.begin && last == c.end) {
-            const float inv = 1.f / l;
-            if (mine) {
-#pragma unroll
-                for (int rr = 0; rr < 4; rr++)
-#pragma unroll
-                    for (int i = 0; i < T; i++) {
-                        const f32x4 lo = w.sums4(rr, 2 * i), hi = w.sums4(rr, 2 * i + 1);
-                        const float o[8] = {lo[0] * inv, lo[1] * inv, lo[2] * inv, lo[3] * inv, hi[0] * inv, hi[1] * inv, hi[2] * inv, hi[3] * inv};
-                        store_out8(a.out, a.out_dtype, ((int64_t)c.b * a.Hq + w.qhead) * D + e0 + 8 * T * rr + 8 * i, o);
-                    }
-            }
+            w.deliver(c.b, l);
             return;
         }
         const int u0 = c.begin / size, u1 = (c.end - 1) / size;
         const Pending p = {c.b, u0, u1 - u0 + 1};
         if (first == t0) head = p;
         else tail = p;
-        if (mine) {
-            const int64_t pi = (int64_t)(share + c.b) * a.Hq + w.qhead;
-            if (e0 == 0) put_partial2<true>((float *)a.part_ml + 2 * pi, (f32x2){w.m, l});
-            float *pa = a.part_acc + pi * D + e0;
-#pragma unroll
-            for (int rr = 0; rr < 4; rr++)
-#pragma unroll
-                for (int i = 0; i < 2 * T; i++) put_partial4<true>(pa + 8 * T * rr + 4 * i, w.sums4(rr, i));
-        }
+        w.put_piece(share + c.b, l);
     };
     // the loader runs DEEP - 1 tiles ahead, across the contexts' borders
     Cursor now, ahead;
@@ -774,9 +844,14 @@ __global__ void __launch_bounds__(512, 2) attn_fp4_share_kernel(const AttnArgs a
         const int begun = (ahead.tile - ahead.begin) * 32;
         w.issue(w.ring + put * Wave::Ring::STAGE, ahead.off + begun, ahead.len - begun);
         put = put + 1 == DEEP ? 0 : put + 1;
-        if (ahead.tile + 1 < ahead.end) ahead.tile++;
-        else if (ahead.tile + 1 < t1) open(ahead, ahead.tile + 1);
-        else ahead.tile++;
+        if (ahead.tile + 1 < ahead.end) {
+            ahead.tile++;
+        } else if (ahead.tile + 1 < t1) {
+            open(ahead, ahead.tile + 1);
+            w.touch_queries(dyn_lds + 8 * DEEP * Wave::Ring::STAGE + ts * 256, ahead.b);
+        } else {
+            ahead.tile++;
+        }
     };
 #pragma unroll
     for (int i = 0; i < DEEP - 1; i++)
@@ -811,12 +886,14 @@ __global__ void __launch_bounds__(512, 2) attn_fp4_share_kernel(const AttnArgs a
     for (int k = 0; k < 2; k++) {
         if (!(who >> k & 1)) continue;
         const Pending p = {k ? tail.b : head.b, k ? tail.first : head.first, k ? tail.count : head.count};
-        const int slices = w.heads * w.per_head * (D / 8);
-        for (int i = w.lane; i < slices; i += 64) {
-            const int c = i / (D / 8), dl = i % (D / 8), sub = NH == 1 ? 0 : c / w.per_head;
-            merge_chunks<D, true>(a, p.first + p.b, a.Hq, p.b, (w.kh0 + sub) * a.group + w.qb * QB + (c - sub * w.per_head), dl, p.count);
-        }
+        w.merge_pieces(p.first + p.b, p.b, p.count);
     }
+}
+
+template <int ACT, int D, int NH, int NP>
+__global__ void __launch_bounds__(512, 2) attn_fp4_share_kernel(const AttnArgs a) {
+    fp4_share<ACT, D, NH, NP>(a);
+    publish_lengths<D>(a);  // (at the end: nothing waits for it)
 }
 
 template <int ACT, int NP, bool SHARES>
@@ -833,7 +910,7 @@ static attn_fn pick_fp4(int d, int nh) {
 attn_fn s3i_pick_fp4(int act, int d, int heads_per_unit, bool wide_out, bool shares, int *lds) {
     const bool wide = d * heads_per_unit == 256;
     const int stage = wide ? Fp4Ring<256>::STAGE : Fp4Ring<128>::STAGE;
-    *lds = shares ? 8 * stage * (wide ? Fp4Ring<256>::DEEP : Fp4Ring<128>::DEEP) : 4 * stage * 2;
+    *lds = shares ? 8 * (stage * (wide ? Fp4Ring<256>::DEEP : Fp4Ring<128>::DEEP) + 256) : 4 * stage * 2;
     if (act == S3_F16) {
         if (wide_out) return shares ? pick_fp4<S3_F16, 3, true>(d, heads_per_unit) : pick_fp4<S3_F16, 3, false>(d, heads_per_unit);
         return shares ? pick_fp4<S3_F16, 2, true>(d, heads_per_unit) : pick_fp4<S3_F16, 2, false>(d, heads_per_unit);

@@ -1136,7 +1136,7 @@ static int launch_fp4(s3_arena *a, const AttnCall &c) {
     const int cus = a->num_cus > 0 ? a->num_cus : 256;
     if (p.shares) {
         args.ncls = 1;
-        const size_t dyn_lds = (((size_t)(c.n + 1) * 4 + 15) & ~(size_t)15) + lds;
+        const size_t dyn_lds = (((size_t)(c.n + 1) * 4 + 15) & ~(size_t)15) + (c.n <= S3_FP4_KNOWN ? (size_t)c.n * 12 : 0) + lds;
         int per_cu = 0;
         rc = resident_per_cu((const void *)fn, 512, dyn_lds, &per_cu);
         if (rc != S3_OK) return rc;
