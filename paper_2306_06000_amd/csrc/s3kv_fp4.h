@@ -18,6 +18,12 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 __host__ __device__ __forceinline__ int fp4_code_bytes(int heads, int d) { return heads * (d / 2); }
 __host__ __device__ __forceinline__ int fp4_scale_bytes(int heads, int d) { return (heads * (d / 32) + 15) & ~15; }
 
+// Two numbers, rounded to bf16 by the conversion instruction (to the nearest, ties to even; NaN stays NaN).
+__device__ __forceinline__ unsigned round_bf16x2(const float x0, const float x1) {
+    const bf16x2 h = {(__bf16)x0, (__bf16)x1};
+    return __builtin_bit_cast(unsigned, h);
+}
+
 // Scale byte of a block whose largest magnitude is `most`: its exponent, one more from 1.75 * 2^k up, less 2.
 template <int ACT>
 __device__ __forceinline__ unsigned fp4_scale_byte(const float most) {

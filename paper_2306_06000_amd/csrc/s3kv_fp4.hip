@@ -177,12 +177,17 @@ __device__ __forceinline__ f16x8 widen_word_f16(const unsigned w, const float sc
 
 // Two fp32 numbers as a word of two bf16 (nearest, ties to even); what that leaves of them stays in x0, x1.
 __device__ __forceinline__ unsigned take_bf16_part(float &x0, float &x1) {
-    const bf16x2 h = {(__bf16)x0, (__bf16)x1};
-    const unsigned w = __builtin_bit_cast(unsigned, h);
+    const unsigned w = round_bf16x2(x0, x1);
     const unsigned lo = w << 16, hi = w & 0xFFFF0000u;
     x0 -= __builtin_bit_cast(float, lo);
     x1 -= __builtin_bit_cast(float, hi);
     return w;
+}
+
+// Eight output elements.
+__device__ __forceinline__ void put_out8(const AttnArgs &a, int64_t e, const float (&v)[8]) {
+    if (a.out_dtype != S3_BF16) return store_out8(a.out, a.out_dtype, e, v);
+    *(u32x4 *)((uint16_t *)a.out + e) = (u32x4){round_bf16x2(v[0], v[1]), round_bf16x2(v[2], v[3]), round_bf16x2(v[4], v[5]), round_bf16x2(v[6], v[7])};
 }
 
 template <int B>
@@ -525,7 +530,7 @@ struct Fp4Wave {
             for (int i = 0; i < T; i++) {
                 const f32x4 lo = sums4(rr, 2 * i), hi = sums4(rr, 2 * i + 1);
                 const float o[8] = {lo[0] * inv, lo[1] * inv, lo[2] * inv, lo[3] * inv, hi[0] * inv, hi[1] * inv, hi[2] * inv, hi[3] * inv};
-                store_out8(a.out, a.out_dtype, ((int64_t)b * a.Hq + qhead) * D + first_element() + 8 * T * rr + 8 * i, o);
+                put_out8(a, ((int64_t)b * a.Hq + qhead) * D + first_element() + 8 * T * rr + 8 * i, o);
             }
     }
 
@@ -579,14 +584,24 @@ struct Fp4Wave {
     }
 };
 
-// The new lengths, and a zero output row for empty or refused contexts, by the workgroups in turn.
+// The new lengths, and a zero output row for empty or refused contexts, by the workgroups in turn.  The first context's entry is asked
+// for when the kernel begins and used when it ends.
+struct FirstEntry {
+    int64_t off;
+    int32_t raw;
+};
+__device__ __forceinline__ FirstEntry first_entry(const AttnArgs &a) {
+    const int b = min((int)blockIdx.x, a.n - 1);
+    return {a.slot_off[b], a.cur_len[b]};
+}
 template <int D>
-__device__ __forceinline__ void publish_lengths(const AttnArgs &a) {
+__device__ __forceinline__ void publish_lengths(const AttnArgs &a, FirstEntry e) {
     for (int b = blockIdx.x; b < a.n; b += gridDim.x) {
-        if (a.len_out && threadIdx.x == 0) a.len_out[b] = a.cur_len[b] + 1;
-        if (checked_len(a, b) == 0) {
+        if (b != (int)blockIdx.x) e = {a.slot_off[b], a.cur_len[b]};
+        if (a.len_out && threadIdx.x == 0) a.len_out[b] = e.raw + 1;
+        if (checked_len(a, e.off, e.raw) == 0) {
             const float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            for (int e = threadIdx.x; e < a.Hq * D / 8; e += blockDim.x) store_out8(a.out, a.out_dtype, ((int64_t)b * a.Hq * D / 8 + e) * 8, z);
+            for (int i = threadIdx.x; i < a.Hq * D / 8; i += blockDim.x) put_out8(a, ((int64_t)b * a.Hq * D / 8 + i) * 8, z);
         }
     }
 }
@@ -603,12 +618,12 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_team_kernel(const AttnArgs a)
     __shared__ float comb_m[TS][16], comb_l[TS][16];
     __shared__ int last_of_context;
     const int ts = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // (scalar: row ranges and buffers with it)
+    const FirstEntry entry = first_entry(a);
     const BatchView bv = build_batch_view<false>(a, dyn_lds, wave_sums);
     char *rings = dyn_lds + ((batch_view_bytes(a.n, a.ncls) + 15) & ~(size_t)15);
     // a wave's ring takes its sums of the columns in use when its rows are done: STRIDE floats a column
     constexpr int RING = 2 * Wave::Ring::STAGE;
     static_assert(16 * STRIDE * 4 <= RING, "a wave's sums fit its ring");
-    publish_lengths<D>(a);
     Wave w(a, rings + ts * RING);
     // Work in the order of eighths: workgroup b (XCD b % 8) takes the chunks whose number leaves the same remainder, so that the
     // columns of a chunk, whose bytes share cache lines, are on one XCD's L2.
@@ -684,7 +699,7 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_team_kernel(const AttnArgs a)
                 const float inv = 1.f / ll;
 #pragma unroll
                 for (int e = 0; e < 8; e++) o[e] *= inv;
-                store_out8(a.out, a.out_dtype, ((int64_t)it.b * a.Hq + h) * D + dl * 8, o);
+                put_out8(a, ((int64_t)it.b * a.Hq + h) * D + dl * 8, o);
             } else {  // a chunk of a longer context: the partial goes out with write-through stores
                 const int64_t pi = (int64_t)(it.slot0 + it.c) * a.Hq + h;
                 if (dl == 0) put_partial2<true>((float *)a.part_ml + 2 * pi, (f32x2){mm, ll});
@@ -712,6 +727,7 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_team_kernel(const AttnArgs a)
         }
         __syncthreads();  // LDS is used again by the next item
     }
+    publish_lengths<D>(a, entry);
 }
 
 // Exclusive prefix sums of the contexts' tiles into pre[0..n], by the whole workgroup; returns the total (longest: the rows of the
@@ -892,8 +908,9 @@ __device__ __forceinline__ void fp4_share(const AttnArgs &a) {
 
 template <int ACT, int D, int NH, int NP>
 __global__ void __launch_bounds__(512, 2) attn_fp4_share_kernel(const AttnArgs a) {
+    const FirstEntry e = first_entry(a);
     fp4_share<ACT, D, NH, NP>(a);
-    publish_lengths<D>(a);  // (at the end: nothing waits for it)
+    publish_lengths<D>(a, e);
 }
 
 template <int ACT, int NP, bool SHARES>

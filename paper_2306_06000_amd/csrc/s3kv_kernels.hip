@@ -838,7 +838,7 @@ static size_t chunk_slots(const s3_arena *a, int n, int n_hg, size_t slot_bytes,
 
 // Rows of 4-bit blocks: how a launch over n contexts is laid out.  A unit is what a wave takes of a row, 128 or 256 elements of one head
 // or of neighbouring ones; a column (of the work list) is a unit and up to sixteen of its query heads.
-#define S3_FP4_SHARES 2
+#define S3_FP4_SHARES 4
 struct Fp4Plan {
     int heads_per_unit, blocks_per_head, columns;
     int counted;    // columns that the arrival counters have room for: the most of any n

@@ -63,7 +63,7 @@ __device__ __forceinline__ u32x4 round8(const float (&y)[8]) {
             const unsigned packed = __builtin_bit_cast(unsigned, h);
             w[i] = packed;
         } else {
-            w[i] = f32_to_bf16_rne(y[2 * i]) | (f32_to_bf16_rne(y[2 * i + 1]) << 16);
+            w[i] = round_bf16x2(y[2 * i], y[2 * i + 1]);
         }
     }
     return w;
