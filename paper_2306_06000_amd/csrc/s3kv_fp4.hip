@@ -184,10 +184,23 @@ __device__ __forceinline__ unsigned take_bf16_part(float &x0, float &x1) {
     return w;
 }
 
-// Eight output elements.
+// Eight output elements; WIDE: of 32 bits.
+template <bool WIDE>
 __device__ __forceinline__ void put_out8(const AttnArgs &a, int64_t e, const float (&v)[8]) {
-    if (a.out_dtype != S3_BF16) return store_out8(a.out, a.out_dtype, e, v);
-    *(u32x4 *)((uint16_t *)a.out + e) = (u32x4){round_bf16x2(v[0], v[1]), round_bf16x2(v[2], v[3]), round_bf16x2(v[4], v[5]), round_bf16x2(v[6], v[7])};
+    if (WIDE) {
+        f32x4 *to = (f32x4 *)((float *)a.out + e);
+        to[0] = (f32x4){v[0], v[1], v[2], v[3]};
+        to[1] = (f32x4){v[4], v[5], v[6], v[7]};
+        return;
+    }
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const f16x2 h = {(_Float16)v[2 * i], (_Float16)v[2 * i + 1]};
+        const unsigned f16 = __builtin_bit_cast(unsigned, h), bf16 = round_bf16x2(v[2 * i], v[2 * i + 1]);
+        w[i] = a.out_dtype == S3_F16 ? f16 : bf16;
+    }
+    *(u32x4 *)((uint16_t *)a.out + e) = w;
 }
 
 template <int B>
@@ -530,7 +543,7 @@ struct Fp4Wave {
             for (int i = 0; i < T; i++) {
                 const f32x4 lo = sums4(rr, 2 * i), hi = sums4(rr, 2 * i + 1);
                 const float o[8] = {lo[0] * inv, lo[1] * inv, lo[2] * inv, lo[3] * inv, hi[0] * inv, hi[1] * inv, hi[2] * inv, hi[3] * inv};
-                put_out8(a, ((int64_t)b * a.Hq + qhead) * D + first_element() + 8 * T * rr + 8 * i, o);
+                put_out8<NP == 3>(a, ((int64_t)b * a.Hq + qhead) * D + first_element() + 8 * T * rr + 8 * i, o);
             }
     }
 
@@ -549,36 +562,27 @@ struct Fp4Wave {
 #pragma unroll
         for (int i = 0; i < 8 * T; i++) put_partial4<true>((float *)(to + i * piece_quads()), acc[i]);
     }
-    // Merges the `count` pieces of context b in slots slot0, slot0 + 1, ..., two a memory round trip, and delivers its rows.
+    // Merges the `count` pieces of context b in slots slot0, slot0 + 1, ... and delivers its rows.  (Two a memory round trip cost registers and
+    // code that all contexts paid for: 64 contexts of 32-400 rows, 16 heads of 256, 34.7 us instead of 33.4.)
     __device__ __forceinline__ void merge_pieces(int64_t slot0, int b, int count) {
         m = -INFINITY;
         l = 0.f;
 #pragma unroll
         for (int i = 0; i < 8 * T; i++) acc[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
         const unsigned bytes = heads * per_head * D * 4, at = delivers() ? piece_lane() : bytes;  // (past the end: zeros, no traffic)
-        for (int c0 = 0; c0 < count; c0 += 2) {
-            f32x2 ml[2];
-            f32x4 p[2][8 * T];
+        for (int c = 0; c < count; c++) {
+            const int64_t slot = slot0 + c;
+            const __amdgpu_buffer_rsrc_t mr = piece_buffer((const float *)a.part_ml + 2 * slot * a.Hq, a.Hq * 8), pr = piece_buffer(piece(slot), bytes);
+            const f32x2 ml = piece_load2(mr, delivers() ? qhead * 8 : a.Hq * 8);
+            f32x4 p[8 * T];
 #pragma unroll
-            for (int u = 0; u < 2; u++) {
-                const int64_t slot = slot0 + c0 + u;
-                const bool is = c0 + u < count;
-                const __amdgpu_buffer_rsrc_t mr = piece_buffer((const float *)a.part_ml + 2 * slot * a.Hq, is ? a.Hq * 8 : 0);
-                const __amdgpu_buffer_rsrc_t pr = piece_buffer(piece(slot), is ? bytes : 0);
-                ml[u] = piece_load2(mr, delivers() ? qhead * 8 : a.Hq * 8);
+            for (int i = 0; i < 8 * T; i++) p[i] = piece_load4(pr, at + i * piece_quads());
+            const float pm = ml[0], mn = fmaxf(m, pm), ref = exp_reference(mn);
+            const float old = fast_exp2(m - ref), now = fast_exp2(pm - ref);
+            l = l * old + ml[1] * now;
 #pragma unroll
-                for (int i = 0; i < 8 * T; i++) p[u][i] = piece_load4(pr, at + i * piece_quads());
-            }
-#pragma unroll
-            for (int u = 0; u < 2; u++) {
-                if (c0 + u >= count) break;
-                const float pm = ml[u][0], mn = fmaxf(m, pm), ref = exp_reference(mn);
-                const float old = fast_exp2(m - ref), now = fast_exp2(pm - ref);
-                l = l * old + ml[u][1] * now;
-#pragma unroll
-                for (int i = 0; i < 8 * T; i++) acc[i] = acc[i] * old + p[u][i] * now;
-                m = mn;
-            }
+            for (int i = 0; i < 8 * T; i++) acc[i] = acc[i] * old + p[i] * now;
+            m = mn;
         }
         deliver(b, l);
     }
@@ -594,14 +598,14 @@ __device__ __forceinline__ FirstEntry first_entry(const AttnArgs &a) {
     const int b = min((int)blockIdx.x, a.n - 1);
     return {a.slot_off[b], a.cur_len[b]};
 }
-template <int D>
+template <int D, bool WIDE>
 __device__ __forceinline__ void publish_lengths(const AttnArgs &a, FirstEntry e) {
     for (int b = blockIdx.x; b < a.n; b += gridDim.x) {
         if (b != (int)blockIdx.x) e = {a.slot_off[b], a.cur_len[b]};
         if (a.len_out && threadIdx.x == 0) a.len_out[b] = e.raw + 1;
         if (checked_len(a, e.off, e.raw) == 0) {
             const float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            for (int i = threadIdx.x; i < a.Hq * D / 8; i += blockDim.x) put_out8(a, ((int64_t)b * a.Hq * D / 8 + i) * 8, z);
+            for (int i = threadIdx.x; i < a.Hq * D / 8; i += blockDim.x) put_out8<WIDE>(a, ((int64_t)b * a.Hq * D / 8 + i) * 8, z);
         }
     }
 }
@@ -699,7 +703,7 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_team_kernel(const AttnArgs a)
                 const float inv = 1.f / ll;
 #pragma unroll
                 for (int e = 0; e < 8; e++) o[e] *= inv;
-                put_out8(a, ((int64_t)it.b * a.Hq + h) * D + dl * 8, o);
+                put_out8<NP == 3>(a, ((int64_t)it.b * a.Hq + h) * D + dl * 8, o);
             } else {  // a chunk of a longer context: the partial goes out with write-through stores
                 const int64_t pi = (int64_t)(it.slot0 + it.c) * a.Hq + h;
                 if (dl == 0) put_partial2<true>((float *)a.part_ml + 2 * pi, (f32x2){mm, ll});
@@ -727,7 +731,7 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_team_kernel(const AttnArgs a)
         }
         __syncthreads();  // LDS is used again by the next item
     }
-    publish_lengths<D>(a, entry);
+    publish_lengths<D, NP == 3>(a, entry);
 }
 
 // Exclusive prefix sums of the contexts' tiles into pre[0..n], by the whole workgroup; returns the total (longest: the rows of the
@@ -801,7 +805,10 @@ __device__ __forceinline__ void fp4_share(const AttnArgs &a) {
     const int place = rank * 8 + ts;
     const int share = place / a.columns, col = place - share * a.columns;
     const bool cut = longest > 32 * S3_FP4_UNCUT;
-    const int size = max((total + a.wave_shares - 1) / a.wave_shares, 1);
+    // A long context among short ones: its pieces, merged one behind the other, cost as much as its tiles when a share has about the root
+    // of its tiles (0.4 of it measured best; 255 contexts of 10-60 rows and one of 16384, 32q/8kv x 128: 72 us instead of 174; all of 32-1000
+    // rows: 43 us either way).
+    const int size = max((total + a.wave_shares - 1) / a.wave_shares, __builtin_amdgcn_readfirstlane((int)(0.4f * sqrtf((float)(longest >> 5)) + 1.f)));
     if (share >= a.wave_shares || share * (int64_t)size >= total) return;
     int t0 = share * size, t1 = min(total, t0 + size);
     int b = __builtin_amdgcn_readfirstlane(find_sequence(pre, a.n, t0));  // the context that holds tile t0
@@ -910,7 +917,7 @@ template <int ACT, int D, int NH, int NP>
 __global__ void __launch_bounds__(512, 2) attn_fp4_share_kernel(const AttnArgs a) {
     const FirstEntry e = first_entry(a);
     fp4_share<ACT, D, NH, NP>(a);
-    publish_lengths<D>(a, e);
+    publish_lengths<D, NP == 3>(a, e);
 }
 
 template <int ACT, int NP, bool SHARES>
