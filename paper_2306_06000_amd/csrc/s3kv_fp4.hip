@@ -1,21 +1,23 @@
 // Kernels for cache rows of 4-bit blocks (S3_MXFP4, s3kv_fp4.h) of libs3kv, gfx950: the append that rounds new rows, and
 // decode attention over the exactly widened codes (section 2.1, in fp32), for any number of query heads per cached head.
 //
-// Attention.  A wave streams tiles of 32 rows of one unit: 128 or 256 elements of a row, i.e. one head of 128 or 256, or two
-// neighbouring heads of 64.  Both products run on the matrix cores (v_mfma_f32_16x16x32_bf16: e2m1 codes under a power of two are
-// exact in bf16) with up to 16 query heads as columns, also for a single one: 17 bits hold four elements, so the vector ALU
-// would need more instructions for them than the memory leaves time for.
-//   S^T = K Q^T   A operand: lane (r, g) holds block g (32 elements, one scale) of row r as it lies in memory, a 16-byte load;
-//                 the four products of a unit of 128 take a word of it each, Q^T in the same element order; beside fp16 queries
-//                 the codes are widened to fp16.
+// Attention.  A wave streams tiles of 32 rows of one unit: 128 or 256 elements of a row, i.e. one head or two or four neighbouring ones.
+// Both products run on the matrix cores (v_mfma_f32_16x16x32: e2m1 codes under a power of two are exact in bf16, and in fp16 but for far
+// scales) with up to 16 query heads as columns, also for a single one: 17 bits hold four elements, so the vector ALU would need more
+// instructions for them than the memory leaves time for.
+//   S^T = K Q^T   A operand: lane (r, g) holds block g (32 elements, one scale) of row r as it lies in memory; the four products of a
+//                 unit of 128 take a word of it each, Q^T in the same element order.  Codes are widened to bf16, beside fp16 queries to
+//                 fp16, so that queries enter as they are; blocks whose scale fp16 does not hold go by way of bf16 parts of the query
+//                 (special_scores).
 //   O^T += V^T P^T  A operand: lane (m, g) holds elements 8m .. 8m+7 (256: 16m ..) of the eight rows 4g .. 4g+3 and 16+4g ..
 //                 16+4g+3 of the tile, one word a row: after widening, pairs of rows are brought together by byte permutes, and
-//                 output tile i gets the elements 8m + i.  No row passes through LDS.  The accumulator layout of S^T is the B
-//                 operand of P^T as it is.  Weights enter as two bf16 parts (2^-17 of a weight off, below a rounding of a 16-bit
-//                 output by 2^5 and more) or, for 32-bit outputs, as three (exact to fp32).
-// The exponent reference of a column follows its maximum lazily (a tile's scores may exceed it by 8 in log2 units), so most
-// tiles need no exchange between lanes.  Four waves of a workgroup split an item's rows, meet in LDS, and chunks of a context
-// meet through memory as in the other kernels.
+//                 output tile i gets the elements 8m + i.  The accumulator layout of S^T is the B operand of P^T as it is.  Weights enter
+//                 as two bf16 parts (2^-17 of a weight off, below a rounding of a 16-bit output by 2^5 and more) or, for 32-bit
+//                 outputs, as three (exact to fp32).
+// The exponent reference of a column follows its maximum lazily (a tile's scores may exceed it by 8 in log2 units), so most tiles need no
+// exchange between lanes.  Rows are read once and go from memory straight into LDS; what bounds long contexts is that stream, what bounds
+// short ones the chain from launch to the first rows (some 6 us), and, for contexts cut in pieces, the meeting of the pieces.  Measured: 512
+// contexts of 512-4096 rows, 32q/8kv x 128, bf16: 218 us, 5.9 TB/s; 256 of 32-1000: 43 us; 1 of 30000: 24 us.
 #include "s3kv_fp4.h"
 
 // grid (n, 2): block (b, which) rounds one new row of `columns` 16-bit elements into row off+pos; a thread has eight elements.
@@ -301,9 +303,9 @@ struct Fp4Wave {
     __device__ __forceinline__ void issue(char *stage, int64_t row, const Offsets &o) const {
         const char *kp = a.kplane + row * code_bytes, *vp = a.vplane + row * code_bytes;
         const char *ks = a.kscale + row * scale_bytes, *vs = a.vscale + row * scale_bytes;
-        // Pieces of 128 bytes carry the streaming hint; of 64, the other half of a cache line is another wave's, which finds it in L2 if
-        // the line was not given up at once (512 contexts of 512..4096 rows, 32q/8kv x 128: 337 us with the hint, 284 without; of 128:
-        // 57 and 61).
+        // Pieces of 128 bytes carry the streaming hint (512 contexts of 512-4096 rows, 32q/8kv x 128: 218 us with it, 249 without); of 64,
+        // the other half of a cache line is another wave's, which finds it in L2 if the line was not given up at once (128 such contexts
+        // by chunks: 113 us with the hint, 106 without).
         constexpr int HINT = W == 256 ? 2 : 0;
 #pragma unroll
         for (int i = 0; i < Ring::LOADS; i++) __builtin_amdgcn_global_load_lds((glb_void *)(kp + o.k[i]), (lds_void *)(stage + i * 1024), 16, 0, HINT);
@@ -360,10 +362,11 @@ struct Fp4Wave {
     }
 
     // Blocks that the products of fold() do not take: with several heads, those that read as NaN, which must not reach the other heads'
-    // columns (NaN times their zeros); beside fp16 queries, those with a scale under which a code is no fp16 number (appended rows have
-    // none: their scales are 101 to 140, or 1 for a block of zeros, and a scale below 104 only where no code is odd).
+    // columns (NaN times their zeros); beside fp16 queries, those with a scale under which a code may be no fp16 number (below 104 half a
+    // step is less than 2^-24).  Appended rows have those only where no number of a block reaches 7 * 2^-24, and 1 for zeros: under 0 and
+    // 1 no number reaches 2^-123, and they count as zeros.
     __device__ __forceinline__ static bool special(unsigned byte) {
-        return ACT == S3_F16 ? byte - 101u > 39u && byte > 1u : NH > 1 && byte == 255u;
+        return ACT == S3_F16 ? byte - 104u > 36u && byte > 1u : NH > 1 && byte == 255u;
     }
     // The scores of a tile with such blocks: head by head, widened to bf16 (fp16 queries are the exact sum of two bf16 parts).
     __device__ __forceinline__ void special_scores(const Fp4Tile<W> &t, f32x4 (&s)[2]) const {
@@ -611,7 +614,8 @@ __device__ __forceinline__ void publish_lengths(const AttnArgs &a, FirstEntry e)
 }
 
 // Few (context, column) pairs: an item is a chunk of a context for a column, its rows shared out over the four waves of a workgroup,
-// which meet in LDS; chunks meet through memory.
+// which meet in LDS; chunks meet through memory.  Units of 128 elements: twice the items of 256, and latency is what counts here (64
+// contexts of 32-400 rows, 32q/8kv x 128: 10 us; in equal shares 26).
 template <int ACT, int D, int NH, int NP>
 __global__ void __launch_bounds__(256, 2) attn_fp4_team_kernel(const AttnArgs a) {
     typedef Fp4Wave<ACT, D, NH, NP> Wave;
@@ -783,7 +787,9 @@ __device__ __forceinline__ int tile_prefix(const AttnArgs &a, int *pre, int64_t 
 // waves end together whatever the lengths, and no wave waits for another.  A share runs through whole contexts, which it finishes by
 // itself, and at either end through a part of one that others share: such a piece goes to memory (share u's piece of context b to slot
 // u + b: along the shares either u or b grows, so no two meet), is counted, and whoever counts the last piece of a context merges them.
-// Contexts of few tiles are not cut: a share takes those that begin in it.
+// Where no context has more than 8 tiles none is cut, a share takes those that begin in it: the meeting would cost more than uneven
+// shares (100-250 rows: 256 contexts, 32q/8kv x 128: 24.8 us, cut 27.2; 1024 contexts, 16q/1kv x 256: 26.6 and 40.3; of up to 13 tiles the
+// former is better cut, 30 and 33 us).
 #define S3_FP4_UNCUT 8
 template <int ACT, int D, int NH, int NP>
 __device__ __forceinline__ void fp4_share(const AttnArgs &a) {

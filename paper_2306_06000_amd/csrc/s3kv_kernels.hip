@@ -838,7 +838,10 @@ static size_t chunk_slots(const s3_arena *a, int n, int n_hg, size_t slot_bytes,
 
 // Rows of 4-bit blocks: how a launch over n contexts is laid out.  A unit is what a wave takes of a row, 128 or 256 elements of one head
 // or of neighbouring ones; a column (of the work list) is a unit and up to sixteen of its query heads.
-#define S3_FP4_SHARES 4
+// Equal shares from 3 contexts and columns a compute unit on.  Shares keep the waves even but cost some 12 us whatever the rows (the batch
+// is looked through, pieces meet in memory): 32q/8kv x 128, shares against chunks, 192 contexts (3) of 10-60, 32-400, 32-1000, 800-2500 rows:
+// 12.3, 27.3, 38.6, 74.6 us against 15.2, 26.6, 40.3, 119.6; 128 contexts (2): 12.0, 25.7, 34.5, 56.6 against 11.3, 17.7, 31.4, 82.1.
+#define S3_FP4_SHARES 3
 struct Fp4Plan {
     int heads_per_unit, blocks_per_head, columns;
     int counted;    // columns that the arrival counters have room for: the most of any n
