@@ -90,7 +90,8 @@ typedef struct {
                           S3_MXFP4: a block's scale is the least power of two under which its largest
                           magnitude is below 7 (at most 2^125; S3_F16: 2^13), its codes the nearest, ties to
                           even, 6 at the most; a block with an infinity or a NaN has scale byte 255 and reads
-                          as NaN.  s3_kv_fill and s3_kv_read_rows move stored rows: the codes of all heads,
+                          as NaN.  Filled rows may hold any scale byte; beside fp16 queries, numbers of K below 2^-123
+                          count as zeros.  s3_kv_fill and s3_kv_read_rows move stored rows: the codes of all heads,
                           [n_kv_heads][head_dim / 2] bytes (element 2i in the low half of byte i), the scale
                           bytes [n_kv_heads][head_dim / 32], zeros up to a multiple of 16 bytes.       */
 } s3_kv_config;
@@ -249,7 +250,9 @@ int s3_kv_fetch(s3_arena *a, int32_t layer, int32_t n, const int64_t *slot_off, 
  * on until the process ends) instead of the arena's scratch: the call makes no hipMalloc, hipFree or other
  * allocating call and never synchronises.  A call that needs more - about
  * n * ceil(max_len / chunk) * n_heads * (4 * head_dim + 8) bytes plus the counters beyond 32 MiB, which hold the
- * 28-layer, 721-sequence GPT-J batch at the default chunk - returns S3_ERR_SCRATCH and launches nothing.
+ * 28-layer, 721-sequence GPT-J batch at the default chunk - returns S3_ERR_SCRATCH and launches nothing.  (4-bit rows: batches of
+ * many contexts need (8 * compute units / units of 256 elements in a row + n) * n_heads * (4 * head_dim + 8) at most, few contexts what is
+ * left and no more.)
  * The "profile" parameter does not time these launches (its events are allocated).  All calls on one GPU,
  * from every arena, share the buffers: the counters, which no partials ever reach, are left at zero by every
  * launch, and partials are always written before they are read, so calls of any arenas and batch sizes may follow
@@ -295,7 +298,9 @@ int s3_kv_compact(s3_arena *a, int32_t n, const int32_t *slot_id, const int32_t 
  * answers S3_ERR_NOMEM, or to make room for others.
  *   s3_kv_evict_bytes  bytes of host memory needed for len rows of every plane (< 0: bad argument)
  *   s3_kv_evict        copies rows [0, len) of K and V of every layer to host_buf (HOST, pinned memory
- *                      makes the copies asynchronous; layout [2*n_layers][len][H][D]) on `stream`, then
+ *                      makes the copies asynchronous; layout [2*n_layers][len][H][D]; S3_MXFP4: the codes of all planes,
+ *                      [2*n_layers][len][H][D/2] bytes, then their scales, [2*n_layers][len] runs of
+ *                      n_kv_heads * head_dim / 32 bytes and zeros up to a multiple of 16) on `stream`, then
  *                      frees the slot.  host_buf is complete once the stream has passed the copies.
  *   s3_kv_restore      reserves a slot for predicted_len (>= len; the paper doubles the old reservation),
  *                      copies the rows back on `stream`; returns the new id / offset / capacity.

@@ -838,10 +838,13 @@ static size_t chunk_slots(const s3_arena *a, int n, int n_hg, size_t slot_bytes,
 
 // Rows of 4-bit blocks: how a launch over n contexts is laid out.  A unit is what a wave takes of a row, 128 or 256 elements of one head
 // or of neighbouring ones; a column (of the work list) is a unit and up to sixteen of its query heads.
-// Equal shares from 3 contexts and columns a compute unit on.  Shares keep the waves even but cost some 12 us whatever the rows (the batch
-// is looked through, pieces meet in memory): 32q/8kv x 128, shares against chunks, 192 contexts (3) of 10-60, 32-400, 32-1000, 800-2500 rows:
-// 12.3, 27.3, 38.6, 74.6 us against 15.2, 26.6, 40.3, 119.6; 128 contexts (2): 12.0, 25.7, 34.5, 56.6 against 11.3, 17.7, 31.4, 82.1.
-#define S3_FP4_SHARES 3
+// Equal shares from 3 contexts and columns a compute unit on, with heads of 256 from 5.  Shares keep the waves even but cost some 12 us
+// whatever the rows (the batch is looked through, pieces meet in memory).  Shares against chunks, us, contexts of 10-60, 32-400, 32-1000,
+// 800-2500 rows: 32q/8kv x 128, 192 contexts (3): 12.3, 27.3, 38.6, 74.6 against 15.2, 26.6, 40.3, 119.6; 128 (2): 12.0, 25.7, 34.5, 56.6
+// against 11.3, 17.7, 31.4, 82.1.  Chunks of heads of 256 are units as wide as a share's, so that a batch has half as many: 16 heads, 80
+// contexts (5) of 10-60, 32-400, 32-1000, 500-1500 rows: 11.9, 36.2, 52.4, 78.1 against 17.2, 29.3, 47.5, 83.8; 64 (4): 11.8, 34.6, 49.9, 66.5
+// against 14.2, 24.3, 42.8, 74.3.
+static int fp4_share_threshold(int head_dim) { return head_dim == 256 ? 5 : 3; }
 struct Fp4Plan {
     int heads_per_unit, blocks_per_head, columns;
     int counted;    // columns that the arrival counters have room for: the most of any n
@@ -868,7 +871,7 @@ static Fp4Plan fp4_plan(const s3_arena *a, int n) {
     p.chunk = a->chunk > 0 ? a->chunk : 1024;
     const size_t slot_bytes = (size_t)a->cfg.n_heads * ((size_t)D * sizeof(float) + sizeof(float2));
     const int64_t most = 8 * cus / p.columns;  // shares of a column: a wave each, eight waves a compute unit
-    p.shares = a->chunk <= 0 && a->grid_blocks <= 0 && p.columns <= 8 * cus && n * (int64_t)p.columns >= S3_FP4_SHARES * cus;
+    p.shares = a->chunk <= 0 && a->grid_blocks <= 0 && p.columns <= 8 * cus && n * (int64_t)p.columns >= fp4_share_threshold(D) * cus;
     p.few = 0;
     if (p.shares) {
         p.slots = (size_t)(most + n);

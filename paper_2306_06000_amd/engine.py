@@ -145,8 +145,8 @@ class DecodeEngine:
         return entry
 
     def kv_dtype_torch(self):
-        """torch type of cache rows handed to fill (8-bit caches: raw codes)."""
-        return torch.uint8 if self.w.dtype == s3.S3_E4M3 else _TORCH_DT[self.w.dtype]
+        """torch type of cache rows handed to fill (8-bit caches: raw codes; 4-bit: rows as they are stored)."""
+        return torch.uint8 if self.w.dtype in (s3.S3_E4M3, s3.S3_MXFP4) else _TORCH_DT[self.w.dtype]
 
     def act_dtype_torch(self):
         """torch type of q, k_new, v_new."""
@@ -554,23 +554,27 @@ class DecodeEngine:
         lengths attention sees): K and V rows read once, q read, out written, new k/v read and
         written."""
         e = 2                    # q, new k and v: 16-bit
-        ec = self.w.elem_bytes   # cache rows
+        row = self.w.row_bytes   # of a cached row
         e_out = {s3.S3_F32: 4, s3.S3_F16: 2, s3.S3_BF16: 2}[self.out_dtype]
         hd = self.w.n_heads * self.w.head_dim
         kvd = self.w.kv_heads * self.w.head_dim  # elements of one cached row
         B = self.n_active
-        return 2 * kvd * ec * int(self.len.sum()) + B * hd * e + B * hd * e_out + 2 * B * kvd * (e + ec)
+        return 2 * row * int(self.len.sum()) + B * hd * e + B * hd * e_out + 2 * B * (kvd * e + row)
 
     def _byte_terms(self):
         """The same count as two factors: bytes per cached row, bytes per sequence (one layer-step)."""
-        e, ec = 2, self.w.elem_bytes
+        e, row = 2, self.w.row_bytes
         e_out = {s3.S3_F32: 4, s3.S3_F16: 2, s3.S3_BF16: 2}[self.out_dtype]
         hd = self.w.n_heads * self.w.head_dim
         kvd = self.w.kv_heads * self.w.head_dim
-        return 2 * kvd * ec, hd * e + hd * e_out + 2 * kvd * (e + ec)
+        return 2 * row, hd * e + hd * e_out + 2 * (kvd * e + row)
 
     def read_slot(self, a, layer, which, n_rows=None):
         n_rows = a.len if n_rows is None else n_rows
+        if self.w.dtype == s3.S3_MXFP4:
+            dst = torch.empty((n_rows, self.w.row_bytes), dtype=torch.uint8, device=self.dev)
+            s3.check(s3.s3_kv_read_rows(self.arena, a.slot, layer, which, 0, n_rows, dst, self._stream_ptr()), "s3_kv_read_rows")
+            return dst.cpu().numpy()
         eight_bit = self.w.dtype == s3.S3_E4M3
         dst = torch.empty((n_rows, self.w.kv_heads, self.w.head_dim), dtype=torch.uint8 if eight_bit else torch.int16,
                           device=self.dev)

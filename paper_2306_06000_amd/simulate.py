@@ -97,4 +97,5 @@ if __name__ == "__main__":
     for pol in ("max", "predicted", "perfect"):
         print(serve(pol))
     print("8-bit rows:", serve("predicted", kv_dtype=s3.S3_E4M3))
+    print("4-bit rows:", serve("predicted", kv_dtype=s3.S3_MXFP4))
     print("4 cached heads for 16 query heads:", serve("predicted", n_kv_heads=4))

@@ -18,6 +18,7 @@ import numpy as np
 SEED_BASE = 230606000
 F16, BF16 = 0, 1
 E4M3 = 3  # 8-bit cache rows (the library's S3_E4M3); queries and new rows keep a 16-bit type
+MXFP4 = 5  # 4-bit cache rows (S3_MXFP4); newcomers' rows, as they are stored, come from the caller
 
 
 def f32_to_f16_bits(x: np.ndarray) -> np.ndarray:
@@ -44,6 +45,8 @@ def f32_to_e4m3_codes(x: np.ndarray) -> np.ndarray:
 def to_bits(x: np.ndarray, dtype: int) -> np.ndarray:
     if dtype == E4M3:
         return f32_to_e4m3_codes(x)
+    if dtype == MXFP4:
+        raise ValueError("4-bit rows are no array of elements")
     return f32_to_f16_bits(x) if dtype == F16 else f32_to_bf16_bits(x)
 
 
@@ -94,6 +97,8 @@ class Workload:
 
     @property
     def elem_bytes(self) -> int:
+        if self.dtype == MXFP4:
+            raise ValueError("4-bit rows: count by row_bytes")
         return 1 if self.dtype == E4M3 else 2
 
     @property
@@ -106,7 +111,10 @@ class Workload:
 
     @property
     def row_bytes(self) -> int:
-        return self.kv_heads * self.head_dim * self.elem_bytes
+        elems = self.kv_heads * self.head_dim
+        if self.dtype == MXFP4:  # codes, a scale byte for 32 of them, up to a multiple of 16
+            return -(-(elems // 2 + elems // 32) // 16) * 16
+        return elems * self.elem_bytes
 
     @property
     def bytes_per_token(self) -> int:
