@@ -627,7 +627,7 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_team_kernel(const AttnArgs a)
     __shared__ int last_of_context;
     const int ts = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // (scalar: row ranges and buffers with it)
     const FirstEntry entry = first_entry(a);
-    const BatchView bv = build_batch_view<false>(a, dyn_lds, wave_sums);
+    const BatchView bv = build_batch_view<false, true>(a, dyn_lds, wave_sums);
     char *rings = dyn_lds + ((batch_view_bytes(a.n, a.ncls) + 15) & ~(size_t)15);
     // a wave's ring takes its sums of the columns in use when its rows are done: STRIDE floats a column
     constexpr int RING = 2 * Wave::Ring::STAGE;
