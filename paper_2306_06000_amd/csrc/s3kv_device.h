@@ -327,13 +327,13 @@ __device__ __forceinline__ int few_chunk_rows(const AttnArgs &a, int total, int 
 }
 
 // The same for 4-bit rows: four waves share a chunk in tiles of 32 rows, hence steps of 128; rows stream faster (a chunk of c rows costs about
-// c / 30 of one more to merge); contexts do not divide evenly, hence n / 2 chunks less.  us, by this rule and by few_chunk_rows: one context
-// of 8034 rows, 32q/8kv x 128: 13.4, 15.0, 16 x 256: 17.8, 22.9; 16 of 100-900, 32q/8kv x 128: 10.9, 13.5; 32 of 32-1000: 12.2, 16.9; 64 of
-// 500-1500, 16q/1kv x 256: 17.8, 26.9.
-__device__ __forceinline__ int few_chunk_rows_fp4(const AttnArgs &a, int total, int longest) {
+// c / merge of one more to merge: 30, 10 where all threads merge); contexts do not divide evenly, hence n / 2 chunks less.  us, by this rule
+// and by few_chunk_rows, whatever the merge: one context of 8034 rows, 32q/8kv x 128: 13.4, 15.0, 16 x 256: 17.8, 22.9; 16 of 100-900,
+// 32q/8kv x 128: 10.9, 13.5; 32 of 32-1000: 12.2, 16.9; 64 of 500-1500, 16q/1kv x 256: 17.8, 26.9.
+__device__ __forceinline__ int few_chunk_rows_fp4(const AttnArgs &a, int total, int longest, int merge) {
     if (longest <= 256) return a.chunk;
     const int even = total / max(a.few_chunks - ((a.n + 1) >> 1), 1) + 1;
-    const int least = (int)__builtin_amdgcn_sqrtf(30.f * (float)longest);
+    const int least = (int)__builtin_amdgcn_sqrtf((float)merge * (float)longest);
     return min(a.chunk, (max(max(even, least), 256) + 127) & ~127);
 }
 
@@ -396,7 +396,7 @@ __device__ __forceinline__ size_t batch_view_bytes(int n, int ncls) {
 
 // The one-wave build of the view: lane l owns entries l*E .. l*E+E-1 (n <= 64*E).  `how`, for the other waves, where
 // the rows decide: rows per chunk, classes, mean rows of a context.
-template <int E, bool UNITS, bool FP4>
+template <int E, bool UNITS, int FP4>
 __device__ __forceinline__ void one_wave_view(const AttnArgs &a, int64_t *off_s, int *len_s, int *pre, int *how) {
     const int lane = threadIdx.x & 63, n = a.n;
     int chunk = a.chunk, ncls = a.ncls, mean = 0;
@@ -419,7 +419,7 @@ __device__ __forceinline__ void one_wave_view(const AttnArgs &a, int64_t *off_s,
 #pragma unroll
         for (int e = 0; e < E; e++) rows += len[e];
         rows = __builtin_amdgcn_readlane(wave_inclusive_scan(rows), 63);
-        if (a.few_chunks > 0) chunk = FP4 ? few_chunk_rows_fp4(a, rows, mx) : few_chunk_rows(a, rows, mx);
+        if (a.few_chunks > 0) chunk = FP4 ? few_chunk_rows_fp4(a, rows, mx, FP4) : few_chunk_rows(a, rows, mx);
         auto chunks_of = [&](int rows_each) {
             int count = 0;
 #pragma unroll
@@ -579,7 +579,7 @@ __device__ __forceinline__ BatchView build_tile_view(const AttnArgs &a, char *dy
 
 // One pass over the device arrays (each entry is read from global memory once and checked once),
 // then class-wise exclusive prefix sums of the chunk counts.
-template <bool UNITS = false, bool FP4 = false>
+template <bool UNITS = false, int FP4 = 0>
 __device__ __forceinline__ BatchView build_batch_view(const AttnArgs &a, char *dyn, int *wave_sums) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int nthreads = blockDim.x, nwaves = nthreads >> 6;

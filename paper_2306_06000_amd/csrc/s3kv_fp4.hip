@@ -17,7 +17,7 @@
 // The exponent reference of a column follows its maximum lazily (a tile's scores may exceed it by 8 in log2 units), so most tiles need no
 // exchange between lanes.  Rows are read once and go from memory straight into LDS; what bounds long contexts is that stream, what bounds
 // short ones the chain from launch to the first rows (some 6 us), and, for contexts cut in pieces, the meeting of the pieces.  Measured: 512
-// contexts of 512-4096 rows, 32q/8kv x 128, bf16: 218 us, 5.9 TB/s; 256 of 32-1000: 43 us; 1 of 30000: 24 us.
+// contexts of 512-4096 rows, 32q/8kv x 128, bf16: 218 us, 5.9 TB/s; 256 of 32-1000: 43 us; 1 of 30000: 18 us.
 #include "s3kv_fp4.h"
 
 // grid (n, 2): block (b, which) rounds one new row of `columns` 16-bit elements into row off+pos; a thread has eight elements.
@@ -613,6 +613,39 @@ __device__ __forceinline__ void publish_lengths(const AttnArgs &a, FirstEntry e)
     }
 }
 
+// Folds chunks c0 .. c1-1 of a context (their pieces begin at piece p0, a row of Hq pieces a chunk) into (m, l, o), eight elements of a head.
+template <int D>
+__device__ __forceinline__ void merge_range(const AttnArgs &a, int64_t p0, int dl, int c0, int c1, float &m, float &l, float (&o)[8]) {
+    for (; c0 < c1; c0 += 4) {
+        const float *mp[4], *ap[4];
+        f32x2 ml[4];
+        f32x4 lo[4], hi[4];
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+            const int64_t at = p0 + (int64_t)min(c0 + u, c1 - 1) * a.Hq;
+            mp[u] = (const float *)a.part_ml + 2 * at;
+            ap[u] = a.part_acc + at * D + dl * 8;
+        }
+        get_partials<true>(mp, ap, ml, lo, hi);
+        const float mn = fmaxf(fmaxf(m, fmaxf(ml[0][0], ml[1][0])), fmaxf(ml[2][0], ml[3][0]));  // (repeats do not change it)
+        const float ref = exp_reference(mn), old = fast_exp2(m - ref);
+        l *= old;
+#pragma unroll
+        for (int i = 0; i < 8; i++) o[i] *= old;
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+            const float w = c0 + u < c1 ? fast_exp2(ml[u][0] - ref) : 0.f;
+            l += w * ml[u][1];
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                o[i] += w * lo[u][i];
+                o[4 + i] += w * hi[u][i];
+            }
+        }
+        m = mn;
+    }
+}
+
 // Few (context, column) pairs: an item is a chunk of a context for a column, its rows shared out over the four waves of a workgroup,
 // which meet in LDS; chunks meet through memory.  Units of 128 elements: twice the items of 256, and latency is what counts here (64
 // contexts of 32-400 rows, 32q/8kv x 128: 10 us; in equal shares 26).
@@ -627,7 +660,7 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_team_kernel(const AttnArgs a)
     __shared__ int last_of_context;
     const int ts = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // (scalar: row ranges and buffers with it)
     const FirstEntry entry = first_entry(a);
-    const BatchView bv = build_batch_view<false, true>(a, dyn_lds, wave_sums);
+    const BatchView bv = build_batch_view<false, W == 256 ? 30 : 10>(a, dyn_lds, wave_sums);
     char *rings = dyn_lds + ((batch_view_bytes(a.n, a.ncls) + 15) & ~(size_t)15);
     // a wave's ring takes its sums of the columns in use when its rows are done: STRIDE floats a column
     constexpr int RING = 2 * Wave::Ring::STAGE;
@@ -727,9 +760,47 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_team_kernel(const AttnArgs a)
             __syncthreads();
             if (last_of_context) {
                 if (a.merge_sync) __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-                for (int i = threadIdx.x; i < slices; i += 256) {
-                    const int c = i / (D / 8), dl = i % (D / 8), sub = NH == 1 ? 0 : c / w.per_head;
-                    merge_chunks<D, true>(a, it.slot0, a.Hq, it.b, (w.kh0 + sub) * a.group + w.qb * QB + (c - sub * w.per_head), dl, it.nchunks);
+                const auto head_of = [&](int c) {
+                    const int sub = NH == 1 ? 0 : c / w.per_head;
+                    return (w.kh0 + sub) * a.group + w.qb * QB + (c - sub * w.per_head);
+                };
+                if (W == 256 || slices > 128 || it.nchunks <= 4) {
+                    for (int i = threadIdx.x; i < slices; i += 256)
+                        merge_chunks<D, true>(a, it.slot0, a.Hq, it.b, head_of(i / (D / 8)), i % (D / 8), it.nchunks);
+                } else {
+                    // Threads left over take chunks of their own, four at least, and meet in LDS (one context of 8034 rows, 32q/8kv x 128: 11.9 us
+                    // instead of 13.7; of 30000: 18 instead of 21.9).  Not beside units of 256 elements, whose loop over the rows, short of
+                    // registers, got a fifth slower by it.
+                    const int parts = min(256 / slices, (it.nchunks + 3) / 4), per = (it.nchunks + parts - 1) / parts;
+                    const int part = threadIdx.x / slices, i = threadIdx.x - part * slices, h = head_of(i / (D / 8)), dl = i % (D / 8);
+                    float *at = (float *)rings;  // [parts][slices] of (max, sum, 8 values, 2 unused)
+                    float mm = -INFINITY, ll = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                    if (part < parts) {
+                        merge_range<D>(a, (int64_t)it.slot0 * a.Hq + h, dl, part * per, min(it.nchunks, (part + 1) * per), mm, ll, o);
+                        float *mine = at + threadIdx.x * 12;
+                        *(f32x4 *)mine = (f32x4){mm, ll, 0.f, 0.f};
+                        *(f32x4 *)(mine + 4) = (f32x4){o[0], o[1], o[2], o[3]};
+                        *(f32x4 *)(mine + 8) = (f32x4){o[4], o[5], o[6], o[7]};
+                    }
+                    __syncthreads();
+                    if (part == 0) {
+                        for (int x = 1; x < parts; x++) {
+                            const float *from = at + (x * slices + i) * 12;
+                            const f32x4 ml = *(const f32x4 *)from, lo = *(const f32x4 *)(from + 4), hi = *(const f32x4 *)(from + 8);
+                            const float mn = fmaxf(mm, ml[0]), ref = exp_reference(mn), old = fast_exp2(mm - ref), now = fast_exp2(ml[0] - ref);
+                            ll = ll * old + ml[1] * now;
+#pragma unroll
+                            for (int e = 0; e < 4; e++) {
+                                o[e] = o[e] * old + lo[e] * now;
+                                o[4 + e] = o[4 + e] * old + hi[e] * now;
+                            }
+                            mm = mn;
+                        }
+                        const float inv = 1.f / ll;
+#pragma unroll
+                        for (int e = 0; e < 8; e++) o[e] *= inv;
+                        put_out8<NP == 3>(a, ((int64_t)it.b * a.Hq + h) * D + dl * 8, o);
+                    }
                 }
             }
         }
