@@ -197,7 +197,8 @@ int s3_decode_step(s3_arena *a, int32_t layer, int32_t n, const int32_t *slot_id
  *   norm      x * 1 / sqrt(mean(x^2) + eps) * weight over the head_dim elements of a head, if a weight is given
  *   rotation  pair i of the first rotary_dim elements, (i, i + rotary_dim/2) or, interleaved, (2i, 2i+1), turns from (a, b) to
  *             (a cos t - b sin t, a sin t + b cos t), t = position * inv_freq[i]; elements from rotary_dim on are not turned
- * Norms, angles and rotation are computed in 32 bits (angles from positions far out in 64) and rounded once.
+ * Norms, angles and rotation are computed in 32 bits (angles from positions far out in 64) and rounded once; a head whose squares
+ * pass the range of 32 bits has a norm beyond measure and becomes zeros.
  * Several axes (time, height, width): pair i turns by the token's position on axis axis_of_pair[i]. */
 typedef struct {
     int32_t rotary_dim;   /* even, 0 (no rotation) .. head_dim                                                    */

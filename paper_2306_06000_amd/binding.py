@@ -218,11 +218,11 @@ def s3_kv_append(arena, layer, n, slot_off, pos, k_new, v_new, stream=0, slot_id
 
 def make_rotary(rotary_dim, inv_freq, interleaved=False, n_axes=1, axis_of_pair=None, q_weight=None, k_weight=None, eps=1e-6):
     """The rule of s3_qk_rotary and s3_kv_append_rotary.  inv_freq, q_weight, k_weight: float32 device tensors (or addresses);
-    axis_of_pair: host sequence.  The rule keeps them alive."""
+    axis_of_pair: host sequence.  Weights hold head_dim elements, which is the caller's to see to.  The rule keeps them alive."""
     axis = None if axis_of_pair is None else np.ascontiguousarray(axis_of_pair, np.uint8)
     if axis is not None and axis.size < int(rotary_dim) // 2:
         raise ValueError(f"axis_of_pair holds {axis.size} of {int(rotary_dim) // 2} pairs")
-    for name, t, size in (("inv_freq", inv_freq, int(rotary_dim) // 2), ("q_weight", q_weight, 1), ("k_weight", k_weight, 1)):
+    for name, t, size in (("inv_freq", inv_freq, int(rotary_dim) // 2), ("q_weight", q_weight, int(rotary_dim)), ("k_weight", k_weight, int(rotary_dim))):
         if hasattr(t, "data_ptr") and (str(t.dtype) != "torch.float32" or t.numel() < size or not t.is_contiguous()):
             raise ValueError(f"{name} must be contiguous float32 with at least {size} elements")
     rule = s3_rotary(int(rotary_dim), int(interleaved), int(n_axes), float(eps), _ptr(inv_freq), _ptr(axis), _ptr(q_weight), _ptr(k_weight))

@@ -202,3 +202,19 @@ def test_replayed_graphs_of_many():
             assert torch.equal(out, want)
         assert torch.equal(rig.attend(q[:3].contiguous(), few, 1, off=rig.off_d[:3]), first)
     rig.close()
+
+
+@pytest.mark.parametrize("grid", [0, 512], ids=["shares", "chunks"])
+@pytest.mark.parametrize("n", [1024, 1025, 4095])
+def test_largest_batches_of_wide_heads(n, grid):
+    """Units of 256 elements need the most LDS beside the view of the batch."""
+    lens = np.random.default_rng(n).integers(0, 70, n).tolist()
+    lens[17] = 900
+    rig = Many(4, 2, 256, 1, [max(L, 1) for L in lens])
+    assert s3.s3_kv_set_param(rig.a, "grid_blocks", grid) == 0
+    rig.fill(lens)
+    q, q64 = numbers(rig.rng, (n, 4, 256), 1)
+    out = rig.attend(q, lens)
+    rig.check_some(out, q64, lens, 2, some(lens))
+    assert (out[rig.lens_d(lens) == 0] == 0).all()
+    rig.close()
