@@ -41,12 +41,14 @@ struct RotaryArgs {
 static bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 
 // sin and cos of 2 pi x, |x| <= 1/2: the nearest quarter of a turn, and Taylor's sums for the rest (at most pi/4; the terms left out
-// are below 2^-29).
-__device__ __forceinline__ void sin_cos_turn(const float x, float &s, float &c) {
-    const float quarter = rintf(4.f * x);
-    const float t = (x - 0.25f * quarter) * 6.28318530717958648f, t2 = t * t;
-    const float ps = t + t * t2 * (-1.f / 6 + t2 * (1.f / 120 + t2 * (-1.f / 5040 + t2 * (1.f / 362880))));
-    const float pc = 1.f + t2 * (-0.5f + t2 * (1.f / 24 + t2 * (-1.f / 720 + t2 * (1.f / 40320 + t2 * (-1.f / 3628800)))));
+// are below 2^-29).  Their first two terms are in 64 bits, so that a result is off by little more than its one rounding: errors of these
+// two are common to a token's heads, and rows of few bits show them as codes beside the nearest (with all in 32 bits, 25 thousand rows of
+// 8-bit keys had 1.5 times the wrong codes).
+__device__ __forceinline__ void sin_cos_turn(const double x, float &s, float &c) {
+    const double quarter = rint(4.0 * x), t = fma(-0.25, quarter, x) * 6.283185307179586477, t2 = t * t;
+    const float u = (float)t2;
+    const float ps = (float)fma(t * t2, (double)(u * (1.f / 120 + u * (-1.f / 5040 + u * (1.f / 362880)))) - 1.0 / 6, t);
+    const float pc = (float)fma(t2, (double)(u * (1.f / 24 + u * (-1.f / 720 + u * (1.f / 40320 + u * (-1.f / 3628800))))) - 0.5, 1.0);
     const int k = (int)quarter & 3;
     s = k & 1 ? pc : ps;
     c = k & 1 ? ps : pc;
@@ -187,7 +189,7 @@ __global__ void __launch_bounds__(256) rotary_kernel(const RotaryArgs a) {
                 double turn = (double)(axis[i] & 2 ? axis[i] & 1 ? where[3] : where[2] : axis[i] & 1 ? where[1] : where[0]) * rate[i];
                 turn -= rint(turn);
                 float s, c;
-                sin_cos_turn((float)turn, s, c);
+                sin_cos_turn(turn, s, c);
                 mine[lane + 64 * i] = (f32x2){c, s};
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
