@@ -126,7 +126,7 @@ __device__ __forceinline__ void read_tile(Fp4Tile<256> &t, unsigned k, unsigned 
         "ds_read_b64 %11, %27 offset:1536\n\t"
         "ds_read_b64 %12, %27 offset:2048\n\t"
         "ds_read_b64 %13, %27 offset:2560\n\t"
-        "ds_read_b64 %14, %27 offset:3072\n\t"
+        "ds_read_b64 %14, %27 offset:0xc00\n\t"
         "ds_read_b64 %15, %27 offset:3584\n\t"
         "ds_read_u8 %16, %28\n\t"
         "ds_read_u8 %17, %28 offset:8\n\t"

@@ -16,7 +16,7 @@ TDT = {0: torch.float16, 1: torch.bfloat16, 2: torch.float32}
 
 @pytest.fixture(scope="module", autouse=True)
 def need_gpu_and_lib():
-    assert torch.cuda.is_available(), "these tests need the GPU box"
+    assert torch.cuda.is_available(), "these tests need a GPU"
     assert os.path.exists(s3.LIB_PATH), "libs3kv.so must be built before the GPU tests run"
     s3.lib()
 
