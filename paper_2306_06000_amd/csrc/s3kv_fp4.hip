@@ -669,7 +669,11 @@ __global__ void __launch_bounds__(256, 2) attn_fp4_team_kernel(const AttnArgs a)
     // Work in the order of eighths: workgroup b (XCD b % 8) takes the chunks whose number leaves the same remainder, so that the
     // columns of a chunk, whose bytes share cache lines, are on one XCD's L2.
     const int64_t total = (int64_t)((bv.total + 7) / 8) * 8 * a.columns;
-    for (int64_t at = blockIdx.x; at < total; at += gridDim.x) {
+    // The list begins with the longest contexts, and every other round goes through the workgroups backwards: who had the longest has the
+    // shortest next (79 contexts of 32-1000 rows, 16 heads of 256: 50.7 -> 45.7 us, 65 of 32q/8kv x 128: 19.0 -> 17.1).
+    for (int64_t from = 0, back = 0; from < total; from += gridDim.x, back ^= 1) {
+        const int64_t at = from + (back ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+        if (at >= total) continue;
         const int64_t y = at >> 3;
         const int64_t chunk_no = (y / a.columns) * 8 + (at & 7);
         if (chunk_no >= bv.total) continue;
