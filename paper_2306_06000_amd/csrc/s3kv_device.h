@@ -328,8 +328,8 @@ __device__ __forceinline__ int few_chunk_rows(const AttnArgs &a, int total, int 
 
 // The same for 4-bit rows: four waves share a chunk in tiles of 32 rows, hence steps of 128; rows stream faster (a chunk of c rows costs about
 // c / merge of one more to merge: 30, 10 where all threads merge); contexts do not divide evenly, hence n / 2 chunks less.  us, by this rule
-// and by few_chunk_rows, whatever the merge: one context of 8034 rows, 32q/8kv x 128: 13.4, 15.0, 16 x 256: 17.8, 22.9; 16 of 100-900,
-// 32q/8kv x 128: 10.9, 13.5; 32 of 32-1000: 12.2, 16.9; 64 of 500-1500, 16q/1kv x 256: 17.8, 26.9.
+// (by few_chunk_rows): one context of 8034 rows, 16 x 256: 17.5 (22.9); 16 of 100-900, 32q/8kv x 128: 10.9 (13.5); 32 of 32-1000: 12.9 (16.9);
+// 64 of 500-1500, 16q/1kv x 256: 18.5 (26.9).
 __device__ __forceinline__ int few_chunk_rows_fp4(const AttnArgs &a, int total, int longest, int merge) {
     if (longest <= 256) return a.chunk;
     const int even = total / max(a.few_chunks - ((a.n + 1) >> 1), 1) + 1;

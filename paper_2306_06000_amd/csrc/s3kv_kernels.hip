@@ -840,10 +840,10 @@ static size_t chunk_slots(const s3_arena *a, int n, int n_hg, size_t slot_bytes,
 // or of neighbouring ones; a column (of the work list) is a unit and up to sixteen of its query heads.
 // Equal shares from 3 contexts and columns a compute unit on, with heads of 256 from 5.  Shares keep the waves even but cost some 12 us
 // whatever the rows (the batch is looked through, pieces meet in memory).  Shares against chunks, us, contexts of 10-60, 32-400, 32-1000,
-// 800-2500 rows: 32q/8kv x 128, 192 contexts (3): 12.3, 27.3, 38.6, 74.6 against 15.2, 26.6, 40.3, 119.6; 128 (2): 12.0, 25.7, 34.5, 56.6
-// against 11.3, 17.7, 31.4, 82.1.  Chunks of heads of 256 are units as wide as a share's, so that a batch has half as many: 16 heads, 80
-// contexts (5) of 10-60, 32-400, 32-1000, 500-1500 rows: 11.9, 36.2, 52.4, 78.1 against 17.2, 29.3, 47.5, 83.8; 64 (4): 11.8, 34.6, 49.9, 66.5
-// against 14.2, 24.3, 42.8, 74.3.
+// 800-2500 rows: 32q/8kv x 128, 192 contexts (3): 12.4, 27.2, 39.0, 77.1 against 14.6, 26.5, 41.5, 117.5; 128 (2): 12.0, 25.7, 34.5, 56.6
+// against 10.8, 17.2, 29.7, 76.9.  Chunks of heads of 256 are units as wide as a share's, so that a batch has half as many: 16 heads, 80
+// contexts (5) of 10-60, 32-400, 32-1000, 500-1500 rows: 12.0, 36.1, 52.8, 79.7 against 17.1, 28.2, 47.9, 84.0; 64 (4): 11.8, 34.6, 49.9, 66.5
+// against 13.5, 24.3, 40.4, 71.8.
 static int fp4_share_threshold(int head_dim) { return head_dim == 256 ? 5 : 3; }
 struct Fp4Plan {
     int heads_per_unit, blocks_per_head, columns;
